@@ -345,6 +345,108 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
                        float* dX1, float* dX2, float* dparams,
                        void* workspace, int64_t workspace_bytes, void* stream);
 
+/* ---- Losses over a vocabulary -----------------------------------------------
+ *
+ * What a training step needs between rev_stack_forward and
+ * rev_stack_backward_*: a linear map from the rows that leave the stack (after
+ * the caller's final normalisation, if any) to the logits of a vocabulary, and
+ * a loss of these, forward and backward.  The paper trains classifiers over
+ * images and text (Sec. 4) and gives no formula; these are the common ones.
+ * With x = X[r] and the logits z_v = <W_v, x> + b_v, v = 0 .. vocab-1:
+ *
+ *   cross entropy   lse = log sum_v exp(z_v),   ce = lse - z_y,   y = labels[r];
+ *   distillation from a teacher of which top_k logits are known, at temperature
+ *   tau:            p_k = softmax over k of teacher_logits[r][k] / tau,
+ *                   lse_tau = log sum_v exp(z_v / tau),
+ *                   kd = tau^2 sum_k p_k (log p_k - (z_{i_k} / tau - lse_tau)),
+ *                   i_k = teacher_idx[r][k]
+ *   (the teacher's distribution is renormalised over the entries given, the
+ *   student's is over the whole vocabulary; several entries of a row may hold
+ *   the same index, their probabilities add).
+ *
+ * The logits of all rows are never kept: the calls go over the vocabulary in
+ * pieces (the forward calls keep two or three statistics of a row and piece),
+ * and a backward call, which takes the log-sum-exps of the forward call,
+ * computes the logits of a piece again.  Its cotangents are the gradients of
+ * the losses of the rows, dloss[r] (1/count for a mean), and it returns
+ *
+ *   dz_v = dloss_ce (exp(z_v - lse) - [v = y])
+ *        + dloss tau (exp(z_v / tau - lse_tau) - sum of p_k over i_k = v),
+ *   dX = dz W,   dW = dz^T X,   db = sum over the rows of dz.
+ *
+ * Rows that do not count.  A label outside [0, vocab) (-100 is usual) is no
+ * label; a teacher entry with an index outside [0, vocab) or a logit of
+ * -infinity is left out.  A row with no label has ce = lse = 0 and one with no
+ * entry kd = lse_tau = 0; a row with neither takes no part: its dX is 0, and
+ * X and the cotangents may hold anything there, infinities and NaN included.
+ * A bias of -infinity, or of the type's lowest value, takes an entry out of
+ * the vocabulary.  If no row counts, dparams is 0.
+ *
+ * Types.  REV_MODE_FP32: everything float32.  REV_MODE_BF16: params, X and dX
+ * bfloat16; dparams float32 or bfloat16 (cfg.grad_mode).  Logits, softmax
+ * statistics and all sums are float32 in both modes; in bf16 mode dz is rounded
+ * to bfloat16 once, as an operand of the two products.  loss, lse, dloss and
+ * teacher_logits float32; labels and teacher_idx int32.
+ *
+ * Packed parameters: W[vocab, d_model] row-major, then b[vocab] if cfg.bias.
+ * dparams: same layout, overwritten.  X, dX: [rows, d_model]; labels, loss,
+ * dloss: [rows]; teacher_idx, teacher_logits: [rows, top_k].  All device
+ * pointers; params, X, dX, dparams 16-byte aligned, the others 4-byte; the
+ * workspace 256-byte aligned and at least rev_vocab_workspace_bytes() long.
+ * Calls enqueue on `stream` and return; nothing is allocated, every region of
+ * the workspace is written before it is read, and calls may be captured into
+ * a HIP graph.  Sums have a fixed order; a row's loss and dX do not depend on
+ * the rows beside it as long as cfg.rows and the number of rows that count stay
+ * the same.
+ *
+ * Limits (REV_EINVAL otherwise): sizes positive; d_model % 8 == 0 and <= 8192;
+ * rows <= 2^20; vocab <= 2^20; 0 <= top_k <= 256; temperature finite and >=
+ * 1/1024 and <= 1024. */
+typedef struct rev_vocab_cfg {
+    int32_t rows;         /* rows of X                                          */
+    int32_t d_model;      /* D: their width                                     */
+    int32_t vocab;        /* V: entries of the vocabulary, any number           */
+    int32_t mode;         /* REV_MODE_FP32 or REV_MODE_BF16                     */
+    int32_t grad_mode;    /* type of dparams; REV_MODE_FP32 unless mode is bf16 */
+    int32_t bias;         /* 1: b[V] behind W, 0: none                          */
+    int32_t top_k;        /* teacher entries per row (distillation calls)       */
+    float   temperature;  /* tau (distillation calls)                           */
+} rev_vocab_cfg;
+
+int     rev_vocab_check_cfg(const rev_vocab_cfg* cfg);
+int64_t rev_vocab_param_count(const rev_vocab_cfg* cfg);       /* V D (+ V) */
+/* Enough for the four calls below with this cfg. */
+int64_t rev_vocab_workspace_bytes(const rev_vocab_cfg* cfg);
+
+/* Softmax cross entropy.  out: loss[rows] (ce), lse[rows]. */
+int rev_xent_forward(const rev_vocab_cfg* cfg, const void* params, const void* X,
+                     const int32_t* labels, float* loss, float* lse,
+                     void* workspace, int64_t workspace_bytes, void* stream);
+/* in: lse of the forward call, dloss[rows]; out: dX, dparams (either may be
+ * null: a frozen map, or rows that need no gradient). */
+int rev_xent_backward(const rev_vocab_cfg* cfg, const void* params, const void* X,
+                      const int32_t* labels, const float* lse, const float* dloss,
+                      void* dX, void* dparams,
+                      void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Distillation (cfg.top_k >= 1), alone (labels null) or with the cross entropy
+ * of labels from the same sweep over the vocabulary.  out: loss_kd[rows],
+ * loss_ce[rows] (null if and only if labels is), lse[2][rows]: lse, then
+ * lse_tau. */
+int rev_distill_forward(const rev_vocab_cfg* cfg, const void* params, const void* X,
+                        const int32_t* labels, const int32_t* teacher_idx,
+                        const float* teacher_logits,
+                        float* loss_ce, float* loss_kd, float* lse,
+                        void* workspace, int64_t workspace_bytes, void* stream);
+/* dloss_ce[rows] (null if and only if labels is) and dloss_kd[rows]: cotangents
+ * of the two losses; dX, dparams as for rev_xent_backward. */
+int rev_distill_backward(const rev_vocab_cfg* cfg, const void* params, const void* X,
+                         const int32_t* labels, const int32_t* teacher_idx,
+                         const float* teacher_logits, const float* lse,
+                         const float* dloss_ce, const float* dloss_kd,
+                         void* dX, void* dparams,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
 /* Per-kernel-family timing.  Between rev_profile_begin() and rev_profile_end()
  * every kernel launch made by the calling process is bracketed by a pair of
  * HIP events on the stream it is launched on.  rev_profile_end() synchronises

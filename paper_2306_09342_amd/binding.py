@@ -28,6 +28,8 @@ EXPORTS = (
     "rev_stack_forward_masked", "rev_stack_backward_reprop_masked", "rev_stack_backward_pareprop_masked",
     "rev_adamw_step", "rev_sgd_step",
     "rev_merge_check_cfg", "rev_merge_param_count", "rev_merge_workspace_bytes", "rev_merge_forward", "rev_merge_backward",
+    "rev_vocab_check_cfg", "rev_vocab_param_count", "rev_vocab_workspace_bytes",
+    "rev_xent_forward", "rev_xent_backward", "rev_distill_forward", "rev_distill_backward",
     "rev_profile_begin", "rev_profile_end", "rev_profile_kinds", "rev_profile_name", "rev_profile_is_flops",
     "rev_profile_get", "rev_last_error",
 )
@@ -43,6 +45,11 @@ class RevMergeCfg(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("grid_h", ctypes.c_int32), ("grid_w", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("d_in", ctypes.c_int32), ("mode", ctypes.c_int32),
                 ("ln_eps", ctypes.c_float), ("fusion", ctypes.c_int32)]
+
+
+class RevVocabCfg(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("d_model", ctypes.c_int32), ("vocab", ctypes.c_int32), ("mode", ctypes.c_int32),
+                ("grad_mode", ctypes.c_int32), ("bias", ctypes.c_int32), ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float)]
 
 
 class RevError(RuntimeError):
@@ -105,6 +112,15 @@ def lib():
         L.rev_merge_forward.restype = ctypes.c_int
         L.rev_merge_backward.argtypes = [mp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp]
         L.rev_merge_backward.restype = ctypes.c_int
+        op = ctypes.POINTER(RevVocabCfg)
+        L.rev_vocab_check_cfg.argtypes = [op]
+        L.rev_vocab_check_cfg.restype = ctypes.c_int
+        for n in ("rev_vocab_param_count", "rev_vocab_workspace_bytes"):
+            getattr(L, n).argtypes = [op]
+            getattr(L, n).restype = i64
+        for n, pointers in (("rev_xent_forward", 5), ("rev_xent_backward", 7), ("rev_distill_forward", 8), ("rev_distill_backward", 10)):
+            getattr(L, n).argtypes = [op] + [vp] * pointers + [vp, i64, vp]
+            getattr(L, n).restype = ctypes.c_int
         for n in ("rev_profile_begin", "rev_profile_end", "rev_profile_kinds"):
             getattr(L, n).argtypes = []
             getattr(L, n).restype = ctypes.c_int
@@ -396,6 +412,111 @@ def rev_merge_backward(cfg, params, X1, X2, dOutA, dOutB, workspace=None, stream
     _check(lib().rev_merge_backward(ctypes.byref(cfg), _ptr(params), _ptr(X1), _ptr(X2), _ptr(dOutA), _ptr(dOutB),
                                     _ptr(dX1), _ptr(dX2), _ptr(dparams), _ptr(ws), ws.numel(), _stream_handle(stream)))
     return {"dX1": dX1, "dX2": dX2, "dparams": dparams}
+
+
+def make_vocab_cfg(rows, d_model, vocab, mode="bf16", grad_mode="fp32", bias=True, top_k=0, temperature=1.0) -> RevVocabCfg:
+    m, gm = (MODES[x] if isinstance(x, str) else int(x) for x in (mode, grad_mode))
+    return RevVocabCfg(rows, d_model, vocab, m, gm, int(bias), top_k, temperature)
+
+
+def rev_vocab_check_cfg(cfg: RevVocabCfg) -> int:
+    return lib().rev_vocab_check_cfg(ctypes.byref(cfg))
+
+
+def rev_vocab_param_count(cfg: RevVocabCfg) -> int:
+    return _check(lib().rev_vocab_param_count(ctypes.byref(cfg)))
+
+
+def rev_vocab_workspace_bytes(cfg: RevVocabCfg) -> int:
+    return _check(lib().rev_vocab_workspace_bytes(ctypes.byref(cfg)))
+
+
+def _vocab_common(cfg, params, X, workspace, floats=(), ints=()):
+    """Checks what the four calls have in common and returns the workspace.  floats, ints: (tensor or None, shape) of float32 and int32."""
+    _want(params, param_dtype(cfg), (rev_vocab_param_count(cfg),))
+    _want(X, param_dtype(cfg), (cfg.rows, cfg.d_model))
+    for dtype, group in ((torch.float32, floats), (torch.int32, ints)):
+        for t, shape in group:
+            if t is not None:
+                _want(t, dtype, shape)
+                assert t.device == X.device, "tensors of different devices"
+    assert params.device == X.device, "tensors of different devices"
+    if workspace is None:
+        return torch.empty(rev_vocab_workspace_bytes(cfg), dtype=torch.uint8, device=X.device)
+    _want(workspace, torch.uint8)
+    return workspace
+
+
+def _vocab_stream(X, stream):
+    return ctypes.c_void_p((torch.cuda.current_stream(X.device) if stream is None else stream).cuda_stream)
+
+
+def _vocab_out(out, name, shape, dtype, X):
+    t = (out or {}).get(name)
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=X.device)
+    _want(t, dtype, shape)
+    return t
+
+
+def _vocab_grads(cfg, X, out, want):
+    assert want and set(want) <= {"dX", "dparams"}, "want: dX, dparams or both"
+    res = {}
+    if "dX" in want:
+        res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X)
+    if "dparams" in want:
+        dtype = torch.bfloat16 if cfg.grad_mode == REV_MODE_BF16 else torch.float32
+        res["dparams"] = _vocab_out(out, "dparams", (rev_vocab_param_count(cfg),), dtype, X)
+    return res
+
+
+def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=None):
+    """Softmax cross entropy of the rows of X over the vocabulary: {"loss", "lse"}, float32 [rows]; labels int32 [rows]."""
+    ws = _vocab_common(cfg, params, X, workspace, ints=[(labels, (cfg.rows,))])
+    loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X) for n in ("loss", "lse"))
+    with torch.cuda.device(X.device):
+        _check(lib().rev_xent_forward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(ws), ws.numel(),
+                                      _vocab_stream(X, stream)))
+    return {"loss": loss, "lse": lse}
+
+
+def rev_xent_backward(cfg, params, X, labels, lse, dloss, workspace=None, stream=None, out=None, want=("dX", "dparams")):
+    """Gradients of sum(dloss * loss), with the lse of the forward call: the members of `want`."""
+    ws = _vocab_common(cfg, params, X, workspace, [(lse, (cfg.rows,)), (dloss, (cfg.rows,))], ints=[(labels, (cfg.rows,))])
+    res = _vocab_grads(cfg, X, out, want)
+    with torch.cuda.device(X.device):
+        _check(lib().rev_xent_backward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(lse), _ptr(dloss), _ptr(res.get("dX")),
+                                       _ptr(res.get("dparams")), _ptr(ws), ws.numel(), _vocab_stream(X, stream)))
+    return res
+
+
+def rev_distill_forward(cfg, params, X, teacher_idx, teacher_logits, labels=None, workspace=None, stream=None, out=None):
+    """Divergence from a teacher's top_k logits (int32 and float32 [rows, top_k]): {"loss", "lse"}, lse float32 [2, rows]; with labels
+    their cross entropy as "loss_ce" too."""
+    top = (cfg.rows, cfg.top_k)
+    ws = _vocab_common(cfg, params, X, workspace, [(teacher_logits, top)], ints=[(labels, (cfg.rows,)), (teacher_idx, top)])
+    res = {"loss": _vocab_out(out, "loss", (cfg.rows,), torch.float32, X), "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X)}
+    if labels is not None:
+        res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X)
+    with torch.cuda.device(X.device):
+        _check(lib().rev_distill_forward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx), _ptr(teacher_logits),
+                                         _ptr(res.get("loss_ce")), _ptr(res["loss"]), _ptr(res["lse"]), _ptr(ws), ws.numel(),
+                                         _vocab_stream(X, stream)))
+    return res
+
+
+def rev_distill_backward(cfg, params, X, teacher_idx, teacher_logits, lse, dloss, labels=None, dloss_ce=None, workspace=None, stream=None,
+                         out=None, want=("dX", "dparams")):
+    """Gradients of sum(dloss * loss) (+ sum(dloss_ce * loss_ce) with labels), with the lse of the forward call."""
+    top, row = (cfg.rows, cfg.top_k), (cfg.rows,)
+    ws = _vocab_common(cfg, params, X, workspace, [(teacher_logits, top), (lse, (2, cfg.rows)), (dloss, row), (dloss_ce, row)],
+                       ints=[(labels, row), (teacher_idx, top)])
+    res = _vocab_grads(cfg, X, out, want)
+    with torch.cuda.device(X.device):
+        _check(lib().rev_distill_backward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx), _ptr(teacher_logits),
+                                          _ptr(lse), _ptr(dloss_ce), _ptr(dloss), _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws),
+                                          ws.numel(), _vocab_stream(X, stream)))
+    return res
 
 
 def rev_profile_begin():

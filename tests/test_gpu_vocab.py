@@ -1,0 +1,294 @@
+"""The losses over a vocabulary on the GPU against the float64 oracle: every output at every element, within what its roundings add up to."""
+import numpy as np
+import pytest
+import torch
+
+import vocab_util as VU
+from paper_2306_09342_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+# rows, width, vocabulary
+SHAPES = [(1, 8, 1), (1, 64, 2), (2, 8, 3), (3, 16, 7), (1, 768, 1003), (5, 128, 257), (16, 72, 300), (33, 200, 255), (64, 384, 1000),
+          (65, 136, 1001), (129, 128, 2049), (200, 256, 513), (257, 64, 770), (300, 384, 1025), (130, 520, 1290), (513, 32, 256)]
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_cross_entropy(shape, mode):
+    M, D, V = shape
+    print("[case] cross entropy", shape, mode, flush=True)
+    VU.check(VU.make(M, D, V, mode, bias=M % 2 == 1, share=1.0 if M < 30 else 0.7, seed=M), "fp32")
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("K,tau", [(1, 1.0), (3, 2.0), (64, 4.0), (65, 0.5), (256, 1.0)])
+@pytest.mark.parametrize("labels", [False, True])
+def test_distillation(K, tau, labels, mode):
+    print("[case] distillation", K, tau, labels, mode, flush=True)
+    VU.check(VU.make(70, 136, 515, mode, bias=labels, K=K, share=0.8, labels=labels, tau=tau, seed=K), "fp32")
+
+
+@pytest.mark.parametrize("shape", [(1, 64, 33), (4, 768, 1001), (300, 320, 1290)])
+def test_distillation_shapes(shape):
+    M, D, V = shape
+    print("[case] distillation", shape, flush=True)
+    VU.check(VU.make(M, D, V, "bf16", K=6, tau=2.0, share=0.9, seed=5), "bf16")
+
+
+def test_bfloat16_gradients_are_the_float32_ones_rounded():
+    c = VU.make(150, 256, 777, "bf16", share=0.6, seed=1)
+    a, b = VU.run(c, "fp32"), VU.run(c, "bf16")
+    assert torch.equal(a["dparams"].bfloat16(), b["dparams"]) and torch.equal(a["dX"], b["dX"])
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("alive", [0, 1, 2])
+def test_few_rows_count(alive, mode):
+    c = VU.make(300, 128, 600, mode, seed=2)
+    keep = c["labels"][:].copy()
+    c["labels"][:] = -1
+    for r in (299, 17)[:alive]:
+        c["labels"][r] = keep[r]
+    c["labels"][5], c["labels"][6], c["labels"][7] = 600, 2 ** 31 - 1, -2 ** 31
+    got, _ = VU.check(c)
+    if alive == 0:
+        assert all(not got[k].any() for k in ("loss_ce", "lse", "dX", "dparams"))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("K", [0, 4])
+def test_rows_that_do_not_count_may_hold_anything(K, mode):
+    c = VU.make(90, 64, 300, mode, K=K, share=0.5, seed=3)
+    ref = VU.run(c)
+    on = (c["labels"] >= 0) | ((c["idx"] >= 0).any(1) if K else False)
+    assert 0 < on.sum() < 90
+    for r in np.nonzero(~on)[0]:
+        c["X"][r] = (np.nan, np.inf, -np.inf)[r % 3]
+        c["dce"][r] = c["dkd"][r] = np.nan
+        if K:
+            c["logits"][r] = np.nan
+    got = VU.run(c)
+    for k in ref:
+        assert torch.equal(ref[k], got[k]), k
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("low", ["-inf", "lowest"])
+def test_entries_taken_out_by_the_bias(low, mode):
+    c = VU.make(80, 64, 1100, mode, seed=4)
+    worst = -np.inf if low == "-inf" else float(torch.finfo(torch.bfloat16 if mode == "bf16" else torch.float32).min)
+    b = c["params"][1100 * 64:]
+    b[0:300] = worst                       # a whole tile of any size, and the first
+    b[301:1090:7] = worst
+    b[1095:] = worst                       # the last
+    keep = np.nonzero(b > -1e30)[0]
+    c["labels"] = np.where(c["labels"] >= 0, keep[np.abs(c["labels"]) % len(keep)], -1).astype(np.int32)
+    VU.check(c)
+
+
+def test_a_label_that_the_bias_took_out():
+    c = VU.make(4, 64, 50, "fp32", seed=6)
+    c["params"][50 * 64 + 7] = -np.inf
+    c["labels"][:] = [7, 3, 7, 9]
+    got = VU.run(c)
+    assert torch.isinf(got["loss_ce"]).cpu().tolist() == [True, False, True, False]
+    assert torch.isfinite(got["dX"]).all() and torch.isfinite(got["dparams"]).all()
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_large_logits(mode):
+    c = VU.make(40, 64, 700, mode, K=3, tau=2.0, seed=7, scale=3000.0)
+    VU.check(c)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_teachers_with_repeats_and_gaps(mode):
+    c = VU.make(12, 64, 90, mode, K=8, tau=1.5, seed=8)
+    c["idx"][0] = 5                                              # one entry, eight times
+    c["idx"][1] = [3, 3, 7, 7, 7, -1, 90, 3]
+    c["logits"][2, :7] = -np.inf                                 # one left
+    c["logits"][3] = -np.inf                                     # none
+    c["idx"][4] = c["labels"][4]                                 # the label too
+    c["labels"][5] = -1
+    c["idx"][6] = -5
+    c["logits"][7] = [100.0, -100.0, 0.0, 99.0, -3e38, 1.0, 2.0, 3.0]
+    c["idx"][8, 0] = 89
+    VU.check(c)
+
+
+def test_a_student_that_is_its_teacher():
+    """The gradient is a difference of two nearly equal probabilities: taken in float32, rounded once."""
+    c = VU.make(20, 64, 120, "bf16", bias=False, K=120, tau=2.0, labels=False, seed=9)
+    W = c["params"].astype(np.float64).reshape(120, 64)
+    c["idx"][:] = np.arange(120)
+    c["logits"] = (c["X"].astype(np.float64) @ W.T * 1.01).astype(np.float32)
+    VU.check(c)
+
+
+@pytest.mark.parametrize("want", [("dX",), ("dparams",)])
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_one_gradient_alone(want, mode):
+    c = VU.make(100, 96, 500, mode, K=2, seed=10)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    f = VU.forward(cfg, c, a)
+    both = VU.backward(cfg, c, a, f["stats"])
+    one = VU.backward(cfg, c, a, f["stats"], want=want)
+    assert set(one) == set(want) and torch.equal(one[want[0]], both[want[0]])
+
+
+@pytest.mark.parametrize("mode,grad", [("bf16", "fp32"), ("bf16", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("shape", [(37, 136, 515), (300, 128, 259), (3, 64, 1001)])
+def test_nothing_is_written_behind_the_outputs_and_the_workspace_may_hold_anything(shape, mode, grad):
+    M, D, V = shape
+    c = VU.make(M, D, V, mode, K=3, share=0.8, seed=11)
+    cfg, a = VU.make_cfg(c, grad), VU.gpu_args(c)
+    ref = VU.run(c, grad)
+    n = B.rev_vocab_workspace_bytes(cfg)
+    outs, pads = {}, []
+
+    def padded(shape, dtype):
+        size = int(np.prod(shape))
+        t = torch.full((size + 64,), 7.0, dtype=dtype, device="cuda")
+        pads.append((t, size))
+        return t[:size].view(shape)
+
+    for fill in (0, 255):
+        ws = torch.full((n + 4096,), fill, dtype=torch.uint8, device="cuda")
+        pads.clear()
+        dt = a["X"].dtype
+        outs = {"loss": padded((M,), torch.float32), "loss_ce": padded((M,), torch.float32), "lse": padded((2, M), torch.float32),
+                "dX": padded((M, D), dt), "dparams": padded((a["params"].numel(),), torch.bfloat16 if grad == "bf16" else torch.float32)}
+        f = VU.forward(cfg, c, a, workspace=ws[:n], out=outs)
+        b = VU.backward(cfg, c, a, f["stats"], workspace=ws[:n], out=outs)
+        torch.cuda.synchronize()
+        assert (ws[n:] == fill).all()
+        for t, size in pads:
+            assert (t[size:] == 7.0).all()
+        for k in ("loss_ce", "loss_kd"):
+            assert torch.equal(f[k], ref[k])
+        for k in ("dX", "dparams"):
+            assert torch.equal(b[k], ref[k])
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_many_rows_of_few_columns(mode):
+    M, D, V = 70001, 8, 5
+    c = VU.make(M, D, V, mode, share=0.5, seed=12)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    f = VU.forward(cfg, c, a)
+    b = VU.backward(cfg, c, a, f["stats"])
+    z = a["X"].double() @ a["params"][:V * D].view(V, D).double().T + a["params"][V * D:].double()
+    y = a["labels"].long()
+    on = y >= 0
+    logp = torch.log_softmax(z, 1)
+    ce = torch.where(on, -logp.gather(1, y.clamp(min=0)[:, None])[:, 0], torch.zeros_like(z[:, 0]))
+    assert torch.allclose(f["loss_ce"].double(), ce, atol=2e-5, rtol=2e-5)
+    dz = (logp.exp() - torch.nn.functional.one_hot(y.clamp(min=0), V)) * (a["dce"].double() * on)[:, None]
+    half = VU.HALF[mode]
+    e = (dz.abs() * half + 1e-5 * dz.abs().amax()).T @ a["X"].double().abs() * 1.1
+    assert ((b["dparams"][:V * D].view(V, D).double() - dz.T @ a["X"].double()).abs() <= e + M * VU.U * (dz.abs().T @ a["X"].double().abs())).all()
+    dX = dz @ a["params"][:V * D].view(V, D).double()
+    assert torch.linalg.norm(b["dX"].double() - dX) <= (4 * half if mode == "bf16" else 2e-5) * torch.linalg.norm(dX)
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_repeats_bit_for_bit_on_any_stream_and_two_at_once(mode):
+    c = VU.make(600, 256, 3001, mode, K=4, share=0.7, tau=2.0, seed=13)
+    ref = VU.run(c, "fp32")
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for s in streams:
+        with torch.cuda.stream(s):
+            ws = torch.empty(B.rev_vocab_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+            f = VU.forward(cfg, c, a, workspace=ws)
+            f.update(VU.backward(cfg, c, a, f["stats"], workspace=ws))
+            got.append((f, ws))
+    torch.cuda.synchronize()
+    for f, _ in got:
+        for k in ref:
+            assert torch.equal(f[k], ref[k]), k
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("M", [4, 300])
+def test_captured_and_replayed_with_other_inputs(M, mode):
+    c = VU.make(M, 128, 1001, mode, K=3, share=0.9, seed=14)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    ws = torch.empty(B.rev_vocab_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    VU.backward(cfg, c, a, VU.forward(cfg, c, a, workspace=ws)["stats"], workspace=ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        f = VU.forward(cfg, c, a, workspace=ws)
+        f.update(VU.backward(cfg, c, a, f["stats"], workspace=ws))
+    for seed in (15, 16, 17):
+        d = VU.make(M, 128, 1001, mode, K=3, share=0.3 * (seed - 14), seed=seed)
+        for k, v in VU.gpu_args(d).items():
+            a[k].copy_(v)
+        g.replay()
+        torch.cuda.synchronize()
+        eager = VU.run(d)
+        for k in eager:
+            assert torch.equal(f[k], eager[k]), (seed, k)
+
+
+def test_a_row_does_not_depend_on_the_rows_beside_it():
+    c = VU.make(400, 128, 2000, "bf16", seed=18)
+    one = VU.run(c)
+    c["X"][200:] = -c["X"][200:]
+    two = VU.run(c)
+    assert torch.equal(one["loss_ce"][:200], two["loss_ce"][:200]) and torch.equal(one["dX"][:200], two["dX"][:200])
+
+
+def test_a_training_step_through_a_stack_and_the_loss():
+    """Forward, loss, gradients of the head, reversible backward, AdamW: together against the oracles."""
+    from oracle import rev_oracle as O
+    from oracle import vocab_oracle as VO
+    from paper_2306_09342_amd import synth
+    cfg = dict(synth.CONFIGS["tiny"], mode="fp32")
+    flat = synth.make_params(cfg, seed=0, perturb=True)
+    x, _, _ = synth.make_inputs(cfg, seed=0)
+    N, T, D, V = cfg["batch"], cfg["seq_len"], cfg["d_model"], 211
+    rng = np.random.default_rng(0)
+    head = (rng.standard_normal(V * D + V) * 0.3).astype(np.float32)
+    labels = rng.integers(0, V, N * T).astype(np.int32)
+    labels[rng.random(N * T) < 0.4] = -100
+    count = int((labels >= 0).sum())
+    # oracles
+    blocks = O.unpack_params(flat.astype(np.float64), cfg["n_blocks"], D, cfg["d_mlp"])
+    y1, y2 = O.stack_forward(x.astype(np.float64), x.astype(np.float64), blocks, cfg["n_heads"])
+    h = ((y1 + y2) / 2).reshape(N * T, D)
+    ref = VO.vocab_loss(head, h, V, True, labels, dce=np.full(N * T, 1.0 / count))
+    dy = ref["dX"].reshape(N, T, D) / 2
+    rdx1, rdx2, rg, _, _ = O.stack_backward_reversible(y1, y2, blocks, cfg["n_heads"], dy, dy)
+    # the framework
+    c, dev = B.make_cfg(**cfg), VU.dev
+    params, X = dev(flat), dev(x)
+    Y1, Y2 = B.rev_stack_forward(c, params, X, X)
+    vc = B.make_vocab_cfg(N * T, D, V, "fp32")
+    H = ((Y1 + Y2) / 2).view(N * T, D)
+    head_gpu = dev(head)
+    f = B.rev_xent_forward(vc, head_gpu, H, dev(labels))
+    g = B.rev_xent_backward(vc, head_gpu, H, dev(labels), f["lse"], torch.full((N * T,), 1.0 / count, device="cuda"))
+    dY = (g["dX"] / 2).view(N, T, D)
+    b = B.rev_stack_backward_pareprop(c, params, Y1, Y2, dY, dY, torch.cuda.Stream())
+    for master, grad in ((params, b["dparams"]), (head_gpu, g["dparams"])):
+        before = master.clone()
+        m, v = torch.zeros_like(master), torch.zeros_like(master)
+        B.rev_adamw_step(master, grad, m, v, 1, lr=1e-3)
+        assert not torch.equal(before, master) and torch.isfinite(master).all()
+    torch.cuda.synchronize()
+
+    def near(got, want, tol=1e-4):
+        got = got.cpu().numpy().astype(np.float64).ravel()
+        want = np.asarray(want).ravel()
+        assert np.abs(got - want).max() <= tol * np.abs(want).max()
+
+    near(f["loss"], ref["loss_ce"])
+    near(g["dparams"], ref["dparams"])
+    near(b["dX1"], rdx1)
+    near(b["dX2"], rdx2)
+    near(b["dparams"], O.pack_params(rg))
