@@ -50,6 +50,7 @@ enum Kind {
     K_OPTIM,         // optimizer update
     K_MIXED,         // launches of small blocks that hold products of several of the families above
     K_LN_PAIR,       // LayerNorm backward of one block with LayerNorm forward of another
+    K_VOCAB,         // products with the weights of a vocabulary
     K_COUNT
 };
 

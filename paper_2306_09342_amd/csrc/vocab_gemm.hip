@@ -1,0 +1,549 @@
+// The products of the losses over a vocabulary in bf16, 256x256 tiles:
+//   logits   z[i, v] = <x_i, W_v> + b_v       x [rows, Dp] and W [V, D] along the contraction; never stored:
+//              forward    a row's maximum and sum of exponentials over half a tile's entries leave the kernel,
+//              backward   dz of a piece of the vocabulary does, in bf16;
+//   dx       dx[i, d] = sum over v of dz[i, v] W[v, d], the vocabulary cut into ranges where there are few tiles;
+//   dw       dW[v, d] = sum over i of dz[i, v] x[i, d].
+//
+// One workgroup of 8 wavefronts per CU, 128 x 64 of the tile per wavefront.  A stage is 64 of the contraction; it travels as four
+// parts of 16 KB (two halves of each operand) through two stages of LDS.  A part is requested again, for the stage after
+// next, as soon as everybody has read it, so seven phases of products pass between a request and its use.  A stage is four phases of
+// one quadrant each; the two wavefronts of a SIMD are half a phase apart, so that one multiplies while the other reads.
+//
+// The number of rows, and what follows from it (tiles, width of a piece, ranges), is read from the device (VocabPlan): a workgroup
+// that finds no tile ends at once.
+#include "mfma.h"
+#include "vocab.h"
+#include <type_traits>
+
+namespace rev {
+
+constexpr int VG_PART = 16384, VG_LDS = 8 * VG_PART;
+template <int V> using vg_int = std::integral_constant<int, V>;
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+struct TileLane {
+    int lane, wave, wm, wn, g, fr;
+    __device__ __forceinline__ TileLane() {
+        lane = threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wm = wave & 1; wn = wave >> 1; g = lane >> 5; fr = lane & 31;
+    }
+    // A wavefront-wide load of an operand that lies along the contraction takes 8 rows of 8 chunks, of one that lies across it 4 rows
+    // of 16 chunks: the row and the byte within it that this lane takes.
+    __device__ __forceinline__ int row_along() const { return wave * 8 + (lane >> 3); }
+    __device__ __forceinline__ int byte_along() const { return ((lane & 7) ^ ((row_along() >> 1) & 7)) << 4; }
+    __device__ __forceinline__ int row_across() const { return wave * 4 + (lane >> 4); }
+    __device__ __forceinline__ int byte_across() const { return ((lane & 15) ^ (4 * (row_across() & 3))) << 4; }
+};
+
+// acc[h][j][i] += the products of B half h (32-entry block i of this wavefront's 64) and A half j over nst stages, an even number,
+// at least two.  Accumulator register v of lane (g, fr) is B entry h 128 + wm 64 + i 32 + 8 (v / 4) + 4 g + v % 4, A entry
+// j 128 + wn 32 + fr.  AKM / BKM: the operand lies across the contraction.  issue_x(half, stage, address in LDS) requests a part.
+template <bool AKM, bool BKM, class IssueA, class IssueB>
+__device__ __forceinline__ void tile_products(unsigned char* smem, const TileLane& t, const IssueA& issue_a, const IssueB& issue_b, int nst,
+                                              f32x16_t (&acc)[2][2][2]) {
+    const unsigned lds0 = (unsigned)(uintptr_t)LDS_PTR(unsigned char, smem), lds_w = lds0 + t.wave * 1024;
+    const int grp = t.wave >> 2;
+    // in LDS B0 B1 of stage 0, B0 B1 of stage 1, then the same of A
+    auto request_b = [&](auto half, int kt) { issue_b(half, kt, lds_w + (kt & 1) * (2 * VG_PART) + decltype(half)::value * VG_PART); };
+    auto request_a = [&](auto half, int kt) { issue_a(half, kt, lds_w + 4 * VG_PART + (kt & 1) * (2 * VG_PART) + decltype(half)::value * VG_PART); };
+    using H0 = vg_int<0>; using H1 = vg_int<1>;
+    request_b(H0{}, 0); request_a(H0{}, 0); request_a(H1{}, 0); request_b(H1{}, 0);
+    request_b(H0{}, 1); request_a(H0{}, 1); request_a(H1{}, 1); request_b(H1{}, 1);
+
+    unsigned a_addr[4], b_addr[4];
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+        const int koff = ((2 * kk + t.g) ^ ((t.fr >> 1) & 7)) << 4;
+        a_addr[kk] = lds0 + 4 * VG_PART + (t.wn * 32 + t.fr) * 128 + koff;
+        b_addr[kk] = lds0 + (t.wm * 64 + t.fr) * 128 + koff;
+    }
+    {
+        const int jj = t.lane & 15, qq = t.lane >> 4, r = (qq >> 1) * 8 + (jj >> 2), c = (qq & 1) * 16 + 4 * (jj & 3);
+        auto at = [&](int col) { return lds0 + r * 256 + (((col >> 3) ^ (4 * (r & 3))) << 4) + (col & 7) * 2; };
+        if (AKM) a_addr[0] = at(t.wn * 32 + c) + 4 * VG_PART;
+        if (BKM) {
+            b_addr[0] = at(t.wm * 64 + c);
+            b_addr[1] = at(t.wm * 64 + 32 + c);
+        }
+    }
+    u32x4_t b0[4][2], b1[4][2], a0[4], a1[4];
+    auto read_tr = [&](unsigned addr, auto off_tag) {
+        constexpr int off = decltype(off_tag)::value;
+        return join64(lds_read_tr16_b64(addr, off), lds_read_tr16_b64(addr, off + 1024));
+    };
+    auto read_b = [&](u32x4_t (&f)[4][2], auto half_tag, auto par_tag) {
+        constexpr int off = decltype(half_tag)::value * VG_PART + decltype(par_tag)::value * (2 * VG_PART);
+        if constexpr (BKM) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                f[0][i] = read_tr(b_addr[i], vg_int<off>{});
+                f[1][i] = read_tr(b_addr[i], vg_int<off + 4096>{});
+                f[2][i] = read_tr(b_addr[i], vg_int<off + 8192>{});
+                f[3][i] = read_tr(b_addr[i], vg_int<off + 12288>{});
+            }
+        } else {
+            f[0][0] = lds_read_b128(b_addr[0], off); f[0][1] = lds_read_b128(b_addr[0], off + 4096);
+            f[1][0] = lds_read_b128(b_addr[1], off); f[1][1] = lds_read_b128(b_addr[1], off + 4096);
+            f[2][0] = lds_read_b128(b_addr[2], off); f[2][1] = lds_read_b128(b_addr[2], off + 4096);
+            f[3][0] = lds_read_b128(b_addr[3], off); f[3][1] = lds_read_b128(b_addr[3], off + 4096);
+        }
+    };
+    auto read_a = [&](u32x4_t (&f)[4], auto half_tag, auto par_tag) {
+        constexpr int off = decltype(half_tag)::value * VG_PART + decltype(par_tag)::value * (2 * VG_PART);
+        if constexpr (AKM) {
+            f[0] = read_tr(a_addr[0], vg_int<off>{});
+            f[1] = read_tr(a_addr[0], vg_int<off + 4096>{});
+            f[2] = read_tr(a_addr[0], vg_int<off + 8192>{});
+            f[3] = read_tr(a_addr[0], vg_int<off + 12288>{});
+        } else {
+            f[0] = lds_read_b128(a_addr[0], off);
+            f[1] = lds_read_b128(a_addr[1], off);
+            f[2] = lds_read_b128(a_addr[2], off);
+            f[3] = lds_read_b128(a_addr[3], off);
+        }
+    };
+    auto pin_b = [&](u32x4_t (&f)[4][2]) {
+        asm volatile("" : "+v"(f[0][0]), "+v"(f[0][1]), "+v"(f[1][0]), "+v"(f[1][1]), "+v"(f[2][0]), "+v"(f[2][1]), "+v"(f[3][0]), "+v"(f[3][1]));
+    };
+    auto pin_a = [&](u32x4_t (&f)[4]) { asm volatile("" : "+v"(f[0]), "+v"(f[1]), "+v"(f[2]), "+v"(f[3])); };
+    auto barrier = [&]() {
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto products = [&](u32x4_t (&fb)[4][2], u32x4_t (&fa)[4], f32x16_t (&c)[2]) {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) c[i] = mfma32(as_bf16x8(fb[kk][i]), as_bf16x8(fa[kk]), c[i]);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // kind 0 requests as it goes; kind 1 is the last stage but one, kind 2 the last.  8 loads of a stage per wavefront, 2 per part.
+    auto stage = [&](auto par_tag, auto kind_tag, int kt) {
+        constexpr int par = decltype(par_tag)::value, kind = decltype(kind_tag)::value;
+        using SP = vg_int<par>; using NP = vg_int<1 - par>;
+        read_a(a0, H0{}, SP{});
+        if (kind == 0) request_b(H0{}, kt + 2);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kind == 0 ? 12 : kind == 1 ? 10 : 2) : "memory");
+        pin_a(a0);
+        barrier();
+        products(b0, a0, acc[0][0]);
+        barrier();
+
+        read_a(a1, H1{}, SP{});
+        if (kind == 0) request_a(H0{}, kt + 2);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kind == 0 ? 12 : kind == 1 ? 8 : 0) : "memory");
+        pin_a(a1);
+        barrier();
+        products(b0, a1, acc[0][1]);
+        barrier();
+
+        read_b(b1, H1{}, SP{});
+        if (kind == 0) request_a(H1{}, kt + 2);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kind == 0 ? 12 : kind == 1 ? 6 : 0) : "memory");
+        pin_b(b1);
+        barrier();
+        products(b1, a1, acc[1][1]);
+        barrier();
+
+        if (kind != 2) read_b(b0, H0{}, NP{});
+        if (kind == 0) request_b(H1{}, kt + 2);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" :: "n"(kind == 0 ? 12 : kind == 1 ? 4 : 0) : "memory");
+        if (kind != 2) pin_b(b0);
+        barrier();
+        products(b1, a0, acc[1][0]);
+        barrier();
+    };
+    wait_vm<12>();                                                 // B0 and A0 of stage 0 have landed
+    barrier();
+    read_b(b0, H0{}, vg_int<0>{});
+    wait_lds();
+    pin_b(b0);
+    barrier();
+    if (grp) barrier();                                            // half a phase behind
+    int kt = 0;
+    for (; kt + 3 < nst; kt += 2) {
+        stage(vg_int<0>{}, vg_int<0>{}, kt);
+        stage(vg_int<1>{}, vg_int<0>{}, kt + 1);
+    }
+    stage(vg_int<0>{}, vg_int<1>{}, kt);
+    stage(vg_int<1>{}, vg_int<2>{}, kt + 1);
+    if (!grp) barrier();
+}
+
+__device__ __forceinline__ void clear(f32x16_t (&acc)[2][2][2]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[h][j][i][v] = 0.f;
+}
+
+constexpr float LOG2E = 1.44269504088896341f;
+
+// The logits of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so that neither
+// costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the sums are of
+// exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are kept side by side.
+// What bounds it: see the file's head; the epilogue is 128 exponentials a lane (twice that with DUAL), which nothing overlaps.
+template <bool GRAD, bool DUAL>
+__global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const TileLane t;
+    const VocabPlan pl = *p.plan;
+    const int tiles_m = __builtin_amdgcn_readfirstlane(pl.rows >> 8);
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.V, v0 = GRAD ? width * p.piece : 0, n = min(width, p.V - v0);
+    const int tiles_n = n > 0 ? (n + 255) >> 8 : 0, tiles = tiles_m * tiles_n;
+    if ((int)blockIdx.x >= tiles) return;
+    const int tile = xcd_remap(blockIdx.x, tiles);
+    const int gn = tiles_n <= 6 ? tiles_n : 4, per_group = gn * tiles_m, tg = tile / per_group, in_grp = tile - tg * per_group;
+    const int gw = min(gn, tiles_n - tg * gn);
+    const int m0 = __builtin_amdgcn_readfirstlane((in_grp / gw) * 256), n0 = __builtin_amdgcn_readfirstlane((tg * gn + in_grp % gw) * 256);
+
+    const int64_t lda = p.Dp, ldb = p.Dp;
+    const unsigned va = (unsigned)(t.row_along() * lda * 2 + t.byte_along());
+    const int last = n - 1 - n0;                                   // rows of W beyond it read that one again
+    const char* a_base = reinterpret_cast<const char*>(p.x + m0 * lda);
+    const char* b_base = reinterpret_cast<const char*>(p.wp + (int64_t)(v0 + n0) * ldb);
+    unsigned vb[2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) vb[h][q] = (unsigned)(min(h * 128 + q * 64 + t.row_along(), last) * ldb * 2 + t.byte_along());
+    auto issue_a = [&](auto half, int kt, unsigned lds) {
+        const char* src = a_base + decltype(half)::value * 256 * lda + kt * 128;
+        dma16_sbase(src, va, lds);
+        dma16_sbase(src + 128 * lda, va, lds + 8192);
+    };
+    auto issue_b = [&](auto half, int kt, unsigned lds) {
+        constexpr int h = decltype(half)::value;
+        const char* src = b_base + kt * 128;
+        dma16_sbase(src, vb[h][0], lds);
+        dma16_sbase(src, vb[h][1], lds + 8192);
+    };
+    f32x16_t acc[2][2][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * (v >> 2) + 4 * t.g + (v & 3);
+                const float b = c >= n ? -INFINITY : p.bias ? to_f(p.bias[v0 + c]) : 0.f;
+                acc[h][0][i][v] = b;
+                acc[h][1][i][v] = b;
+            }
+    tile_products<false, false>(smem, t, issue_a, issue_b, p.Dp >> 6, acc);
+
+    if constexpr (!GRAD) {
+        const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
+        const int strip = (n0 >> 7) + t.wm;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float m = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[h][j][i][v]);
+            m = fmaxf(m, __shfl_xor(m, 32, 64));
+            const float ref = m == -INFINITY ? 0.f : m;
+            float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float d = acc[h][j][i][v] - ref;     // first: a lowest value times a scale may overflow
+                        s0 += __builtin_amdgcn_exp2f(d * e0);
+                        if (DUAL) s1 += __builtin_amdgcn_exp2f(d * e1);
+                    }
+            s0 += __shfl_xor(s0, 32, 64);
+            if (DUAL) s1 += __shfl_xor(s1, 32, 64);
+            if (t.g == 0) {
+                float* out = p.stats + (int64_t)strip * (DUAL ? 3 : 2) * p.Mp + m0 + j * 128 + t.wn * 32 + t.fr;
+                out[0] = m;
+                out[p.Mp] = s0;
+                if (DUAL) out[2 * p.Mp] = s1;
+            }
+        }
+    } else {
+        const int64_t ldz = width;
+        const float s0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = m0 + j * 128 + t.wn * 32 + t.fr;
+            // rows behind the last one that counts: 0 exp(z - infinity)
+            float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
+            if (row < pl.count) c = p.coef[row];
+            if (!DUAL && (p.losses & LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
+            bf16* out = p.dz + row * ldz + n0 + t.wm * 64 + 8 * t.g;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    unsigned w[4][2];                              // [v / 4][pair]
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            float d[2];
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const float z = acc[h][j][i][4 * q + 2 * k + u];
+                                d[u] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
+                                if (DUAL) d[u] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[u]);
+                            }
+                            typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+                            const bf16x2_t b = {(__bf16)d[0], (__bf16)d[1]};
+                            w[q][k] = __builtin_bit_cast(unsigned, b);
+                        }
+                    // lanes g = 0 and 1 hold entries 0..3 and 4..7 of every eight; exchanged, each has all of one eight: g = 0 of the first of
+                    // a pair of eights, g = 1 of the second
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        const u32x2_t x0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
+                        const u32x2_t x1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
+                        *reinterpret_cast<u32x4_t*>(out + h * 128 + i * 32 + 8 * q) = u32x4_t{x0[0], x1[0], x0[1], x1[1]};
+                    }
+                }
+        }
+    }
+}
+
+// dx of 256 rows and 256 columns over a range of a piece of the vocabulary, in float32, to a place of the range's own, in the order of
+// the accumulators (dx_of_fragments reads it); later pieces add to it.
+__global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const TileLane t;
+    const VocabPlan pl = *p.plan;
+    const int tiles_d = (p.D + 255) >> 8, tiles = __builtin_amdgcn_readfirstlane((pl.rows >> 8) * tiles_d);
+    const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
+    if (n <= 0 || (int)blockIdx.x >= tiles * pl.splits) return;
+    const int lin = xcd_remap(blockIdx.x, tiles * pl.splits);
+    const int split = __builtin_amdgcn_readfirstlane(lin / tiles), tile = __builtin_amdgcn_readfirstlane(lin - split * tiles);
+    const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
+    const int st0 = split * __builtin_amdgcn_readfirstlane(pl.stages), nst = min(__builtin_amdgcn_readfirstlane(pl.stages), ((n + 127) >> 7) * 2 - st0);
+    float* out = p.acc + (int64_t)lin * 65536 + t.wave * 8192 + t.lane * 4;
+    f32x16_t acc[2][2][2];
+    clear(acc);
+    if (nst > 0) {
+        const int64_t lda = width, ldb = p.D;
+        const unsigned va = (unsigned)(t.row_along() * lda * 2 + t.byte_along());
+        const char* a_base = reinterpret_cast<const char*>(p.dz + m0 * lda + st0 * 64);
+        const char* b_base = reinterpret_cast<const char*>(p.w + (int64_t)v0 * ldb + n0);
+        unsigned col[2];                                           // columns beyond D read the last eight again (never used)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) col[h] = (unsigned)min(h * 256 + t.byte_across(), (p.D - 8 - n0) * 2);
+        const unsigned vrow = (unsigned)(t.row_across() * ldb * 2);
+        auto issue_a = [&](auto half, int kt, unsigned lds) {
+            const char* src = a_base + decltype(half)::value * 256 * lda + kt * 128;
+            dma16_sbase(src, va, lds);
+            dma16_sbase(src + 128 * lda, va, lds + 8192);
+        };
+        auto issue_b = [&](auto half, int kt, unsigned lds) {
+            constexpr int h = decltype(half)::value;
+            const int k0 = (st0 + kt) * 64;
+            if (k0 + 64 <= n) {
+                const char* src = b_base + k0 * ldb * 2;
+                dma16_sbase(src, vrow + col[h], lds);
+                dma16_sbase(src + 64 * ldb, vrow + col[h], lds + 8192);
+            } else {                                               // rows beyond the piece, where dz is 0, read its last one
+                const int first = min(k0, n - 1), left = n - 1 - first;
+                const char* src = b_base + first * ldb * 2;
+                dma16_sbase(src, (unsigned)(min(t.row_across(), left) * ldb * 2) + col[h], lds);
+                dma16_sbase(src, (unsigned)(min(t.row_across() + 32, left) * ldb * 2) + col[h], lds + 8192);
+            }
+        };
+        tile_products<false, true>(smem, t, issue_a, issue_b, nst, acc);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16_t& c = acc[h][j][i];
+                    f32x4_t v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+                    f32x4_t* at = reinterpret_cast<f32x4_t*>(out + ((h * 4 + j * 2 + i) * 4 + q) * 256);
+                    if (p.piece > 0) v += *at;
+                    *at = v;
+                }
+}
+
+// dX[r], 32 columns per thread: the ranges' sums of the row's place added in order; zeros for a row that does not count.
+__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const int* __restrict__ place, int M, bf16* __restrict__ dX) {
+    const int blocks = (p.D + 31) >> 5, r = blockIdx.x * 64 + (threadIdx.x & 63), cb = blockIdx.y * 4 + (threadIdx.x >> 6);
+    if (r >= M || cb >= blocks) return;
+    const int i = place[r], d0 = cb * 32;
+    f32x4_t s[8] = {};
+    if (i >= 0) {
+        const VocabPlan pl = *p.plan;
+        const int tiles_d = (p.D + 255) >> 8, tiles = (pl.rows >> 8) * tiles_d, tile = (i >> 8) * tiles_d + (d0 >> 8);
+        const int h = d0 >> 7 & 1, wm = d0 >> 6 & 1, ib = d0 >> 5 & 1, j = i >> 7 & 1, wn = i >> 5 & 3, fr = i & 31;
+        const float* at = p.acc + (int64_t)tile * 65536 + (wn * 2 + wm) * 8192 + (h * 4 + j * 2 + ib) * 1024 + fr * 4;
+        for (int k = 0; k < pl.splits; ++k) {
+            const float* q = at + (int64_t)k * tiles * 65536;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += *reinterpret_cast<const f32x4_t*>(q + (e >> 1) * 256 + (e & 1) * 128);
+        }
+    }
+    bf16* out = dX + (int64_t)r * p.D + d0;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2)
+        if (d0 + e * 4 < p.D) {
+            typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+            bf16x8 b;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { b[k] = (__bf16)s[e][k]; b[4 + k] = (__bf16)s[e + 1][k]; }
+            *reinterpret_cast<bf16x8*>(out + e * 4) = b;
+        }
+}
+
+// dW of 256 entries of a piece and 256 columns over all rows, and, in the workgroups behind the tiles, db of 256 entries each: these
+// find the CUs that the last round of tiles leaves idle.
+template <typename TG>
+__global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dparams, int db) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const TileLane t;
+    const VocabPlan pl = *p.plan;
+    const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
+    if (n <= 0) return;
+    const int tiles_v = (n + 255) >> 8, tiles_d = (p.D + 255) >> 8, tiles = tiles_v * tiles_d;
+    const int64_t ldz = width;
+    if ((int)blockIdx.x >= tiles) {
+        const int b = blockIdx.x - tiles;
+        if (!db || b >= tiles_v) return;
+        const int c = threadIdx.x & 31, lane_row = threadIdx.x >> 5;
+        float s[8] = {};
+        const bf16* src = p.dz + b * 256 + c * 8;
+        for (int r = lane_row; r < pl.count; r += 16) {
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(src + r * ldz);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[2 * e] += __uint_as_float(v[e] << 16);
+                s[2 * e + 1] += __uint_as_float(v[e] & 0xFFFF0000u);
+            }
+        }
+        float* sh = reinterpret_cast<float*>(smem);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sh[lane_row * 256 + c * 8 + e] = s[e];
+        __syncthreads();
+        if (threadIdx.x < 256 && b * 256 + (int)threadIdx.x < n) {
+            float sum = 0.f;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) sum += sh[k * 256 + threadIdx.x];
+            dparams[(int64_t)p.V * p.D + v0 + b * 256 + threadIdx.x] = from_f<TG>(sum);
+        }
+        return;
+    }
+    const int tile = xcd_remap(blockIdx.x, tiles);
+    const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
+    const int nst = __builtin_amdgcn_readfirstlane(((pl.count + 127) >> 7) * 2);
+    f32x16_t acc[2][2][2];
+    clear(acc);
+    if (nst > 0) {
+        const int64_t ldb = p.Dp;
+        const unsigned va = (unsigned)(t.row_across() * ldz * 2 + t.byte_across());
+        unsigned vb[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) vb[h] = (unsigned)(t.row_across() * ldb * 2 + min(h * 256 + t.byte_across(), (p.Dp - 8 - n0) * 2));
+        const char* a_base = reinterpret_cast<const char*>(p.dz + m0);
+        const char* b_base = reinterpret_cast<const char*>(p.x + n0);
+        auto issue_a = [&](auto half, int kt, unsigned lds) {
+            const char* src = a_base + decltype(half)::value * 256 + kt * 128 * ldz;
+            dma16_sbase(src, va, lds);
+            dma16_sbase(src + 64 * ldz, va, lds + 8192);
+        };
+        auto issue_b = [&](auto half, int kt, unsigned lds) {
+            const char* src = b_base + kt * 128 * ldb;
+            dma16_sbase(src, vb[decltype(half)::value], lds);
+            dma16_sbase(src + 64 * ldb, vb[decltype(half)::value], lds + 8192);
+        };
+        tile_products<true, true>(smem, t, issue_a, issue_b, nst, acc);
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int v = m0 + j * 128 + t.wn * 32 + t.fr;
+        TG* out = dparams + (int64_t)(v0 + v) * p.D + n0 + t.wm * 64;
+        if constexpr (sizeof(TG) == 4) {
+            if (v >= n) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x16_t& c = acc[h][j][i];
+                        const int d = h * 128 + i * 32 + 8 * q + 4 * t.g;
+                        if (n0 + t.wm * 64 + d < p.D)
+                            *reinterpret_cast<f32x4_t*>(out + d) = f32x4_t{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+                    }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    unsigned w[4][2];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+                            const bf16x2_t b = {(__bf16)acc[h][j][i][4 * q + 2 * k], (__bf16)acc[h][j][i][4 * q + 2 * k + 1]};
+                            w[q][k] = __builtin_bit_cast(unsigned, b);
+                        }
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2) {
+                        const u32x2_t x0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
+                        const u32x2_t x1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
+                        const int d = h * 128 + i * 32 + 8 * q + 8 * t.g;
+                        if (v < n && n0 + t.wm * 64 + d < p.D) *reinterpret_cast<u32x4_t*>(out + d) = u32x4_t{x0[0], x1[0], x0[1], x1[1]};
+                    }
+                }
+        }
+    }
+}
+
+template <typename... A>
+static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipStream_t s, A... args) {
+    if (int rc = lim.ensure(reinterpret_cast<const void*>(kern), VG_LDS)) return rc;
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(512), VG_LDS, s, args...);
+    REV_HIP(hipGetLastError());
+    return REV_OK;
+}
+
+int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+    static LdsLimit lim[4];
+    if (grad) return dual ? launch_tiles(vocab_logits_kernel<true, true>, lim[0], blocks, s, p) : launch_tiles(vocab_logits_kernel<true, false>, lim[1], blocks, s, p);
+    return dual ? launch_tiles(vocab_logits_kernel<false, true>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false>, lim[3], blocks, s, p);
+}
+int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+    static LdsLimit lim;
+    return launch_tiles(vocab_dx_kernel, lim, blocks, s, p);
+}
+int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, bf16* dX) {
+    ProfScope ps(K_REDUCE, s, 6.0 * M * p.D);
+    hipLaunchKernelGGL(vocab_dx_rows_kernel, dim3((M + 63) / 64, ((p.D + 31) / 32 + 3) / 4), dim3(256), 0, s, p, place, M, dX);
+    REV_HIP(hipGetLastError());
+    return REV_OK;
+}
+int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+    static LdsLimit lim[2];
+    if (grad_bf16) return launch_tiles(vocab_dw_kernel<bf16>, lim[0], blocks, s, p, (bf16*)dparams, (int)db);
+    return launch_tiles(vocab_dw_kernel<float>, lim[1], blocks, s, p, (float*)dparams, (int)db);
+}
+
+}  // namespace rev

@@ -16,10 +16,30 @@
 
 namespace rev {
 
+// What bounds a plan: floats of dz, tiles of 256 columns in dx, places for its ranges (0, 0, 0: the float32 products, which have none).
+struct PlanLimits { int64_t dz; int tiles_d, slots; };
+struct RowResults { float* p[4]; };
+
+// Pieces of equal widths whose dz fits.  dx has few tiles: its contraction, the piece, is cut into the number of ranges that keeps the
+// 256 CUs busiest; a range costs about 10 stages besides its own (first loads, and writing and reading 256 KB).
+__device__ __forceinline__ VocabPlan plan_of(int count, int V, const PlanLimits& lim) {
+    VocabPlan p = {count, (count + 255) / 256 * 256, (V + 255) / 256 * 256, 1, 2};
+    if (lim.dz == 0 || count == 0) return p;                       // (without rows: one piece of zeros for dW)
+    const int64_t most = lim.dz / p.rows / 256 * 256, pieces = (V + most - 1) / most;
+    p.width = (int)((V + pieces - 1) / pieces + 255) / 256 * 256;
+    const int tiles = p.rows / 256 * lim.tiles_d, pairs = p.width / 128;
+    int64_t best = 1ll << 62;
+    for (int s = 1; s <= 64 && s <= pairs && tiles * s <= lim.slots; ++s) {
+        const int64_t cost = (int64_t)((tiles * s + 255) / 256) * ((pairs + s - 1) / s * 2 + 10);
+        if (cost < best) { best = cost; p.splits = s; p.stages = (pairs + s - 1) / s * 2; }
+    }
+    return p;
+}
+
 // ---------------------------------------------------------------------------------
 // which rows count
 // ---------------------------------------------------------------------------------
-constexpr int HAS_LABEL = 1, HAS_TEACHER = 2;
+constexpr int HAS_LABEL = LOSS_CE, HAS_TEACHER = LOSS_KD;
 __device__ __forceinline__ bool in_vocab(int v, int V) { return (unsigned)v < (unsigned)V; }
 __device__ __forceinline__ bool teacher_counts(int idx, float logit, int V) { return in_vocab(idx, V) && !(logit == -INFINITY); }
 
@@ -34,9 +54,11 @@ __global__ __launch_bounds__(256) void row_flags_kernel(const int* __restrict__ 
     if (lane == 0) flags[r] = (labels && in_vocab(labels[r], V) ? HAS_LABEL : 0) | (taught ? HAS_TEACHER : 0);
 }
 
-// One workgroup: list[i] = the i-th row that counts, place[r] = i or -1, *count.  Each thread takes 16 rows at a time.
+// One workgroup: list[i] = the i-th row that counts, place[r] = i or -1, zeros in the results of the others, and the plan.  Each
+// thread takes 16 rows at a time.
 __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict__ labels, const uint8_t* __restrict__ flags, int M, int V,
-                                                           int* __restrict__ list, int* __restrict__ place, int* __restrict__ count) {
+                                                           int* __restrict__ list, int* __restrict__ place, RowResults zero, PlanLimits lim,
+                                                           VocabPlan* __restrict__ plan) {
     __shared__ int wsum[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
@@ -66,17 +88,23 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict
             if (r >= M) break;
             const bool on = mask >> k & 1;
             place[r] = on ? i : -1;
-            if (on) list[i++] = r;
+            if (on) {
+                list[i++] = r;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    if (zero.p[q]) zero.p[q][r] = 0.f;
+            }
         }
         base += total;
         __syncthreads();
     }
-    if (tid == 0) *count = base;
+    if (tid == 0) *plan = plan_of(base, V, lim);
 }
 
 // Xc[i] = X[list[i]], padded with zeros to Dp columns and to all of Mp rows.  Chunks of 16 bytes, one per thread.
 template <typename T>
-__global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ X, const int* __restrict__ list, const int* __restrict__ count,
+__global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ X, const int* __restrict__ list, const VocabPlan* __restrict__ plan,
                                                           int D, int Dp, int64_t chunks, T* __restrict__ Xc) {
     constexpr int E = 16 / sizeof(T);
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -85,8 +113,19 @@ __global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ 
     const int64_t i = c / per;
     const int d = (int)(c - i * per) * E;
     uint4 v = make_uint4(0, 0, 0, 0);
-    if (i < *count && d < D) v = *reinterpret_cast<const uint4*>(X + (int64_t)list[i] * D + d);
+    if (i < plan->count && d < D) v = *reinterpret_cast<const uint4*>(X + (int64_t)list[i] * D + d);
     *reinterpret_cast<uint4*>(Xc + i * Dp + d) = v;
+}
+
+// The rows of W, padded with zeros to Dp columns (a multiple of 128, which the bf16 product over them needs).
+__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16* __restrict__ w, int D, int Dp, int64_t chunks, bf16* __restrict__ out) {
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (c >= chunks) return;
+    const int64_t i = c / (Dp / 8);
+    const int d = (int)(c - i * (Dp / 8)) * 8;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (d < D) v = *reinterpret_cast<const uint4*>(w + i * D + d);
+    *reinterpret_cast<uint4*>(out + i * Dp + d) = v;
 }
 
 // ---------------------------------------------------------------------------------
@@ -103,14 +142,23 @@ __device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
 }
 
 // zs[i][e] = <W_v, x> + b_v.  One workgroup per row, one wavefront per entry at a time.  Bound by reading the rows of W,
-// scattered over all of it.
+// scattered over all of it.  In the backward pass also what the row's dense part is made of.
+struct Cotangents { const float *lse, *lse_tau, *dce, *dkd; };
 template <typename T>
 __global__ __launch_bounds__(256) void sparse_logits_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ Xc, int D, int Dp,
-                                                            float* __restrict__ zs) {
+                                                            float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
+                                                            float4* __restrict__ coef) {
     constexpr int E = 16 / sizeof(T);
     const int i = blockIdx.x;
-    if (i >= *v.count) return;
+    if (i >= v.plan->count) return;
     const int lane = threadIdx.x & 63, r = v.list[i];
+    if (coef && threadIdx.x == 0) {
+        const int f = flags ? flags[r] : HAS_LABEL;
+        float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
+        if (f & HAS_LABEL) { c.x = cot.dce[r]; c.y = cot.lse[r]; }
+        if (f & HAS_TEACHER) { c.z = cot.dkd[r] / v.inv_tau; c.w = cot.lse_tau[r]; }
+        coef[i] = c;
+    }
     const T* x = Xc + (int64_t)i * Dp;
     for (int e = threadIdx.x >> 6; e <= v.K; e += 4) {
         const int n = entry_of(v, r, e);
@@ -158,78 +206,93 @@ __device__ __forceinline__ Teacher teacher_of(const VocabRows& v, int r, int lan
 // ---------------------------------------------------------------------------------
 // losses
 // ---------------------------------------------------------------------------------
-// One wavefront per row of X: the statistics of its pieces joined, the losses, and zeros for what a row has not.
-// stats: [pieces][3][Mp] = maximum, sum of exp(z - maximum), sum of exp((z - maximum) / tau).
-__global__ __launch_bounds__(256) void losses_kernel(VocabRows v, const float* __restrict__ stats, int pieces, int64_t Mp,
-                                                     const float* __restrict__ zs, float* __restrict__ loss_ce, float* __restrict__ loss_kd,
-                                                     float* __restrict__ lse, float* __restrict__ lse_tau) {
-    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= v.M) return;
-    const int i = v.place[r];
-    float ce = 0.f, kd = 0.f, l0 = 0.f, l1 = 0.f;
-    if (i >= 0) {
-        float m = -INFINITY;
-        for (int p = lane; p < pieces; p += 64) m = fmaxf(m, stats[(int64_t)p * 3 * Mp + i]);
-        m = wave_max(m);
-        float s0 = 0.f, s1 = 0.f;
-        for (int p = lane; p < pieces; p += 64) {
-            const float* q = stats + (int64_t)p * 3 * Mp + i;
-            const float d = q[0] - m;
-            s0 += q[Mp] * expf(d);
-            if (loss_kd) s1 += q[2 * Mp] * expf(d * v.inv_tau);
-        }
-        s0 = wave_sum(s0);
-        s1 = wave_sum(s1);
-        const float* z = zs + (int64_t)i * (v.K + 1);
-        const bool has = entry_of(v, r, 0) >= 0;
-        if (has) {
-            l0 = m + logf(s0);
-            ce = logf(s0) + (m - z[0]);
-        }
-        if (loss_kd) {
-            const Teacher t = teacher_of(v, r, lane);
-            if (t.log_norm != -INFINITY) {
-                l1 = m * v.inv_tau + logf(s1);
-                float sum = 0.f;
+// The statistics of 64 rows that count joined, and their losses.  stats: [strips][N][Mp] = maximum m of a strip, sums of
+// exp(z - m) and exp((z - m) / tau), the second with N = 3 only, the first in its place if only the teacher's loss is wanted.  A lane
+// per row and 16 wavefronts over the strips; then a wavefront per row over the teacher's entries.
+template <int N>
+__global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t Mp, const float* __restrict__ zs,
+                                                      const uint8_t* __restrict__ flags, RowResults out) {
+    __shared__ float sh[3][16][64];
+    __shared__ float row[3][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, count = v.plan->count;
+    float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
+    if (i0 >= count) return;
+    const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
+    float m = -INFINITY, s0 = 0.f, s1 = 0.f;
+    const float* at = stats + i0 + lane;
+    if (i0 + lane < count)
+        for (int p0 = w; p0 < strips; p0 += 64) {
+            float a[4][N];
 #pragma unroll
-                for (int q = 0; q < 4; ++q)
-                    if (t.p[q] != 0.f) sum += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - m) * v.inv_tau - logf(s1)));
-                kd = wave_sum(sum) / (v.inv_tau * v.inv_tau);
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int k = 0; k < N; ++k) a[u][k] = p0 + 16 * u < strips ? at[((int64_t)(p0 + 16 * u) * N + k) * Mp] : k ? 0.f : -INFINITY;
+            const float top = fmaxf(fmaxf(fmaxf(a[0][0], a[1][0]), fmaxf(a[2][0], a[3][0])), m);
+            if (top == -INFINITY) continue;
+            s0 *= expf((m - top) * rate0);
+            if (N == 3) s1 *= expf((m - top) * v.inv_tau);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                s0 += a[u][1] * expf((a[u][0] - top) * rate0);
+                if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - top) * v.inv_tau);
             }
+            m = top;
         }
+    sh[0][w][lane] = m; sh[1][w][lane] = s0; sh[2][w][lane] = s1;
+    __syncthreads();
+    if (w == 0) {
+        float top = -INFINITY, t0 = 0.f, t1 = 0.f;
+        for (int k = 0; k < 16; ++k) top = fmaxf(top, sh[0][k][lane]);
+        for (int k = 0; k < 16; ++k) {
+            const float d = sh[0][k][lane] - top;
+            t0 += sh[1][k][lane] * expf(d * rate0);
+            if (N == 3) t1 += sh[2][k][lane] * expf(d * v.inv_tau);
+        }
+        row[0][lane] = top; row[1][lane] = logf(t0); row[2][lane] = logf(N == 3 ? t1 : t0);
     }
-    if (lane == 0) {
-        if (loss_ce) loss_ce[r] = ce;
-        lse[r] = l0;
-        if (loss_kd) { loss_kd[r] = kd; lse_tau[r] = l1; }
+    __syncthreads();
+    if (w == 0 && i0 + lane < count) {
+        const int i = i0 + lane, r = v.list[i];
+        const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
+        if (loss_ce) loss_ce[r] = has ? row[1][lane] + (row[0][lane] - zs[(int64_t)i * (v.K + 1)]) : 0.f;
+        lse[r] = has ? row[0][lane] + row[1][lane] : 0.f;
+    }
+    if (!loss_kd) return;
+    for (int k = w; k < 64 && i0 + k < count; k += 16) {
+        const int i = i0 + k, r = v.list[i];
+        const float top = row[0][k], log_s = row[2][k];
+        float kd = 0.f, l = 0.f;
+        if (flags[r] & HAS_TEACHER) {
+            const float* z = zs + (int64_t)i * (v.K + 1);
+            const Teacher t = teacher_of(v, r, lane);
+            l = top * v.inv_tau + log_s;
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (t.p[q] != 0.f) kd += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - top) * v.inv_tau - log_s));
+            kd = wave_sum(kd) / (v.inv_tau * v.inv_tau);
+        }
+        if (lane == 0) { loss_kd[r] = kd; lse_tau[r] = l; }
     }
 }
 
 // ---------------------------------------------------------------------------------
 // gradient of the logits
 // ---------------------------------------------------------------------------------
-// coef[i] = {dloss_ce or 0, lse, dloss tau or 0, lse_tau}: what a row's dense part is made of.
-__global__ __launch_bounds__(256) void coef_kernel(VocabRows v, const uint8_t* __restrict__ flags, const float* __restrict__ lse,
-                                                   const float* __restrict__ lse_tau, const float* __restrict__ dce,
-                                                   const float* __restrict__ dkd, float4* __restrict__ coef) {
-    const int i = blockIdx.x * 256 + threadIdx.x;
-    if (i >= *v.count) return;
-    const int r = v.list[i], f = flags ? flags[r] : HAS_LABEL;
-    float4 c = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (f & HAS_LABEL) { c.x = dce[r]; c.y = lse[r]; }
-    if (f & HAS_TEACHER) { c.z = dkd[r] / v.inv_tau; c.w = lse_tau[r]; }
-    coef[i] = c;
-}
-
-// dz at the entries v0 .. v0 + n - 1 that a row names, again.  One wavefront per row; an entry that is named several times is written by
-// the first of them.
+// dz at the entries of a piece that a row names, again.  One wavefront per row; an entry that is named several times is written by
+// the first of them.  The piece: n entries from v0, or with n = 0 number v0 of the plan.
 template <typename T>
 __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float* __restrict__ zs, const float4* __restrict__ coef, int v0, int n,
                                                         T* __restrict__ dz, int64_t ld) {
     __shared__ int names[4][257];
     __shared__ float probs[4][257];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * 4 + w;
-    const bool live = i < *v.count;
+    const bool live = i < v.plan->count;
+    if (n == 0) {
+        ld = v.plan->width;
+        v0 *= (int)ld;
+        n = min((int)ld, v.V - v0);
+        if (n <= 0) return;
+    }
     int mine[5];
     if (live) {
         const int r = v.list[i];
@@ -266,33 +329,18 @@ __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float
     }
 }
 
-// dX[r] from the sums of its place, zeros for a row that does not count.
-template <typename T>
-__global__ __launch_bounds__(256) void scatter_dx_kernel(const float* __restrict__ acc, const int* __restrict__ place, int M, int D,
-                                                         T* __restrict__ dX) {
-    const int per = D / 4;
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= (int64_t)M * per) return;
-    const int64_t r = c / per;
-    const int d = (int)(c - r * per) * 4, i = place[r];
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (i >= 0) v = load4(acc + (int64_t)i * D + d);
-    store4(dX + r * D + d, v);
-}
-
 // ---------------------------------------------------------------------------------
-// a piece of the vocabulary with its logits in float32
+// float32: a piece of the vocabulary with its logits in memory
 // ---------------------------------------------------------------------------------
 // One workgroup per row: maximum and sums of a piece (n entries, pitch ld).
-template <typename T>
-__global__ __launch_bounds__(256) void piece_stats_kernel(const float* __restrict__ z, int64_t ld, int n, const T* __restrict__ bias,
-                                                          const int* __restrict__ count, float inv_tau, int64_t Mp, float* __restrict__ stats) {
+__global__ __launch_bounds__(256) void piece_stats_kernel(const float* __restrict__ z, int64_t ld, int n, const float* __restrict__ bias,
+                                                          const VocabPlan* __restrict__ plan, float inv_tau, int64_t Mp, float* __restrict__ stats) {
     __shared__ float sh[3][4];
     const int i = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (i >= *count) return;
+    if (i >= plan->count) return;
     const float* row = z + (int64_t)i * ld;
     float m = -INFINITY;
-    for (int c = threadIdx.x; c < n; c += 256) m = fmaxf(m, row[c] + (bias ? to_f(bias[c]) : 0.f));
+    for (int c = threadIdx.x; c < n; c += 256) m = fmaxf(m, row[c] + (bias ? bias[c] : 0.f));
     m = wave_max(m);
     if (lane == 0) sh[0][w] = m;
     __syncthreads();
@@ -300,7 +348,7 @@ __global__ __launch_bounds__(256) void piece_stats_kernel(const float* __restric
     const float ref = m == -INFINITY ? 0.f : m;
     float s0 = 0.f, s1 = 0.f;
     for (int c = threadIdx.x; c < n; c += 256) {
-        const float d = row[c] + (bias ? to_f(bias[c]) : 0.f) - ref;
+        const float d = row[c] + (bias ? bias[c] : 0.f) - ref;
         s0 += expf(d);
         s1 += expf(d * inv_tau);
     }
@@ -315,44 +363,51 @@ __global__ __launch_bounds__(256) void piece_stats_kernel(const float* __restric
     }
 }
 
-// The dense part of dz, zeros in the columns behind the piece and the rows behind the last one that counts.
-template <typename T>
-__global__ __launch_bounds__(256) void piece_dz_kernel(const float* z, int64_t ld, int n, const T* __restrict__ bias,
-                                                       const int* __restrict__ count, const float4* __restrict__ coef, float inv_tau, int64_t ldz,
-                                                       T* dz) {
+// The dense part of dz in the place of the logits, zeros in the columns behind the piece and the rows behind the last one that counts.
+__global__ __launch_bounds__(256) void piece_dz_kernel(float* z, int64_t ld, int n, const float* __restrict__ bias, const VocabPlan* __restrict__ plan,
+                                                       const float4* __restrict__ coef, float inv_tau) {
     const int across = (int)((ld + 255) / 256), i = blockIdx.x / across, c = (blockIdx.x - i * across) * 256 + threadIdx.x;
     if (c >= ld) return;
     float d = 0.f;
-    if (i < *count && c < n) d = dense_dz(coef[i], z[(int64_t)i * ld + c] + (bias ? to_f(bias[c]) : 0.f), inv_tau);
-    dz[(int64_t)i * ldz + c] = from_f<T>(d);
+    if (i < plan->count && c < n) d = dense_dz(coef[i], z[(int64_t)i * ld + c] + (bias ? bias[c] : 0.f), inv_tau);
+    z[(int64_t)i * ld + c] = d;
 }
 
-// Column sums of a piece of dz, one thread per column.
-template <typename T>
-__global__ __launch_bounds__(256) void piece_colsum_kernel(const T* __restrict__ dz, int64_t ld, int n, const int* __restrict__ count,
-                                                           void* out, int64_t at, bool out_bf16) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= n) return;
+// Column sums of a piece of dz: 64 columns per workgroup, 16 wavefronts over the rows.
+__global__ __launch_bounds__(1024) void piece_colsum_kernel(const float* __restrict__ dz, int64_t ld, int n, const VocabPlan* __restrict__ plan,
+                                                            float* __restrict__ out) {
+    __shared__ float sh[16][64];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, count = plan->count;
     float s = 0.f;
-    for (int i = 0; i < *count; ++i) s += to_f(dz[(int64_t)i * ld + c]);
-    if (out_bf16) reinterpret_cast<bf16*>(out)[at + c] = from_f<bf16>(s);
-    else reinterpret_cast<float*>(out)[at + c] = s;
+    if (c < n)
+        for (int i = w; i < count; i += 16) s += dz[(int64_t)i * ld + c];
+    sh[w][lane] = s;
+    __syncthreads();
+    if (w == 0 && c < n) {
+        for (int k = 1; k < 16; ++k) s += sh[k][lane];
+        out[c] = s;
+    }
 }
 
 __global__ __launch_bounds__(256) void add_kernel(const float* __restrict__ more, int64_t n, float* __restrict__ acc) {
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (c < n) acc[c] += more[c];
 }
-template <typename T>
-__global__ __launch_bounds__(256) void copy_rows_kernel(const T* __restrict__ src, int64_t valid, int64_t total, T* __restrict__ dst) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c < total) dst[c] = c < valid ? src[c] : from_f<T>(0.f);
+__global__ __launch_bounds__(256) void copy_kernel(const float* __restrict__ src, int valid, int total, float* __restrict__ dst) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < total) dst[c] = c < valid ? src[c] : 0.f;
 }
-__global__ __launch_bounds__(256) void store_grad_kernel(const float* __restrict__ src, int64_t n, void* out, int64_t at, bool out_bf16) {
+
+// dX[r] from the sums of its place, zeros for a row that does not count.
+__global__ __launch_bounds__(256) void dx_rows_kernel(const float* __restrict__ acc, const int* __restrict__ place, int M, int D, float* __restrict__ dX) {
+    const int per = D / 4;
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= n) return;
-    if (out_bf16) reinterpret_cast<bf16*>(out)[at + c] = from_f<bf16>(src[c]);
-    else reinterpret_cast<float*>(out)[at + c] = src[c];
+    if (c >= (int64_t)M * per) return;
+    const int64_t r = c / per;
+    const int d = (int)(c - r * per) * 4, i = place[r];
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (i >= 0) v = load4(acc + (int64_t)i * D + d);
+    store4(dX + r * D + d, v);
 }
 
 // ---------------------------------------------------------------------------------
@@ -377,45 +432,62 @@ static int vocab_check(const rev_vocab_cfg* c) {
 }
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+// dz of a piece: 256 MB, what the memory-side cache holds, or 256 entries of all rows if that is more
+constexpr int64_t VOCAB_DZ_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t flags, place, list, count, coef, zs, stats, xc, w, z, dz, acc, dw, wg, total;
-    int64_t Mp, wg_elems;
-    int Dp, Vc, rest, pieces;        // width of a piece, what is left over behind whole multiples of 8, pieces in all
+    int64_t plan, flags, place, list, coef, zs, stats, xc, w, dz, acc, more, total;
+    int64_t Mp;
+    int Dp, strips, pieces;          // bf16: most pieces that a plan may have
+    int Vc, rest;                    // float32: width of a piece, entries left over behind whole multiples of 4 (the last piece)
+    PlanLimits lim;
 };
 static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     VocabLayout L = {};
-    const int64_t M = c.rows, D = c.d_model, V = c.vocab, es = c.mode == REV_MODE_BF16 ? 2 : 4;
-    L.Mp = up(M, 64);
-    L.Dp = c.d_model;
-    const int64_t whole = V / 8 * 8;
-    L.Vc = (int)std::min<int64_t>(std::max<int64_t>((int64_t)(256 << 20) / 4 / L.Mp / 256 * 256, 1024), up(std::max<int64_t>(whole, 8), 8));
-    L.rest = (int)(V - whole);
-    L.pieces = (int)((whole + L.Vc - 1) / L.Vc) + (L.rest ? 1 : 0);
+    const bool wide = c.mode == REV_MODE_BF16;
+    const int64_t M = c.rows, D = c.d_model, V = c.vocab;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
-    L.count = take(4);
+    L.plan = take(sizeof(VocabPlan));
     L.flags = take(M);
     L.place = take(4 * M);
     L.list = take(4 * M);
-    L.coef = take(16 * L.Mp);
     L.zs = take(4 * M * (c.top_k + 1));
-    L.stats = take(12 * L.Mp * L.pieces);
-    L.xc = take(es * L.Mp * L.Dp);
-    L.w = take(es * 8 * D);
-    L.z = take(4 * L.Mp * L.Vc);
-    L.dz = take(es * L.Mp * L.Vc);
-    L.acc = take(4 * L.Mp * D);
-    L.dw = take(4 * std::max<int64_t>(L.Vc, L.Mp) * D);
-    if (es == 2) {
-        const int K = c.d_model, widths[3] = {L.Vc, whole % L.Vc ? (int)(whole % L.Vc) : L.Vc, 8};
-        for (int n : widths) L.wg_elems = std::max(L.wg_elems, wgrad_scratch_elems((int)L.Mp, &n, &K, 1));
+    if (wide) {
+        L.Mp = up(M, 256);
+        L.Dp = (int)up(D, 128);
+        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2, L.Mp * 256), L.Mp * up(V, 256));
+        L.lim.tiles_d = (int)((D + 255) / 256);
+        L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
+        const int64_t least = L.lim.dz / L.Mp / 256 * 256;
+        L.pieces = (int)((V + least - 1) / least);
+        L.strips = (int)((V + 255) / 256) * 2;
+        L.coef = take(16 * M);
+        L.stats = take(12 * L.Mp * L.strips);
+        L.xc = take(2 * L.Mp * L.Dp);
+        L.w = L.Dp != D ? take(2 * V * L.Dp) : 0;
+        L.dz = take(2 * L.lim.dz);
+        L.acc = take((int64_t)L.lim.slots * 65536 * 4);
+    } else {
+        L.Mp = up(M, 64);
+        L.Dp = c.d_model;
+        const int64_t whole = V / 4 * 4;
+        L.Vc = (int)std::min(std::max(VOCAB_DZ_BYTES / 4 / L.Mp / 256 * 256, (int64_t)256), std::max<int64_t>(whole, 4));
+        L.rest = (int)(V - whole);
+        L.pieces = L.strips = (int)((whole + L.Vc - 1) / L.Vc) + (L.rest ? 1 : 0);
+        L.coef = take(16 * M);
+        L.stats = take(12 * L.Mp * L.strips);
+        L.xc = take(4 * L.Mp * D);
+        L.w = take(4 * 4 * D);
+        L.dz = take(4 * L.Mp * L.Vc);
+        L.acc = take(4 * L.Mp * D);
+        L.more = take(4 * std::max<int64_t>(4, L.pieces > 1 ? L.Mp : 0) * D);
     }
-    L.wg = take(4 * L.wg_elems);
     L.total = at;
     return L;
 }
 
 #define RC(expr) do { int _rc = (expr); if (_rc != REV_OK) return _rc; } while (0)
+#define LAUNCH(kern, grid, block, ...) do { hipLaunchKernelGGL(kern, grid, block, 0, s, __VA_ARGS__); REV_HIP(hipGetLastError()); } while (0)
 static dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + per - 1) / per)); }
 
 template <typename T>
@@ -432,120 +504,126 @@ struct VocabRunner {
     VocabRunner(const rev_vocab_cfg& cfg, const void* p, void* w, hipStream_t st, const int* labels, const int* idx, const float* logits)
         : c(cfg), L(vocab_layout(cfg)), ws((char*)w), params((const T*)p), s(st) {
         M = c.rows; D = c.d_model; V = c.vocab;
-        v = {labels, idx, logits, at<int>(L.list), at<int>(L.place), at<int>(L.count), M, V, idx ? c.top_k : 0, c.bias,
+        v = {labels, idx, logits, at<int>(L.list), at<int>(L.place), at<VocabPlan>(L.plan), M, V, idx ? c.top_k : 0, c.bias,
              idx ? 1.f / c.temperature : 1.f};
     }
     template <typename U> U* at(int64_t off) const { return reinterpret_cast<U*>(ws + off); }
     const uint8_t* flags() const { return v.idx ? at<uint8_t>(L.flags) : nullptr; }
     const T* bias() const { return c.bias ? params + (int64_t)V * D : nullptr; }
+    int losses() const { return (v.labels ? LOSS_CE : 0) | (v.idx ? LOSS_KD : 0); }
+    bool dual() const { return losses() == (LOSS_CE | LOSS_KD) && c.temperature != 1.f; }
 
-    int prepare(const void* X) {
+    // the rows that count, their logits at named entries, and in the backward pass (cot.lse) what their dense parts are made of
+    int prepare(const void* X, const RowResults& zero, const Cotangents& cot) {
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
-        if (v.idx) {
-            hipLaunchKernelGGL(row_flags_kernel, blocks_of(M, 4), dim3(256), 0, s, v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
-            REV_HIP(hipGetLastError());
-        }
-        hipLaunchKernelGGL(select_rows_kernel, dim3(1), dim3(1024), 0, s, v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place),
-                           at<int>(L.count));
-        REV_HIP(hipGetLastError());
+        if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
+        LAUNCH(select_rows_kernel, dim3(1), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
         const int64_t chunks = L.Mp * L.Dp * sizeof(T) / 16;
-        hipLaunchKernelGGL(gather_rows_kernel<T>, blocks_of(chunks, 256), dim3(256), 0, s, (const T*)X, at<int>(L.list), at<int>(L.count), D, L.Dp,
-                           chunks, at<T>(L.xc));
-        REV_HIP(hipGetLastError());
-        hipLaunchKernelGGL(sparse_logits_kernel<T>, dim3(M), dim3(256), 0, s, v, params, at<T>(L.xc), D, L.Dp, at<float>(L.zs));
-        REV_HIP(hipGetLastError());
+        LAUNCH(gather_rows_kernel<T>, blocks_of(chunks, 256), dim3(256), (const T*)X, at<int>(L.list), v.plan, D, L.Dp, chunks, at<T>(L.xc));
+        LAUNCH(sparse_logits_kernel<T>, dim3(M), dim3(256), v, params, at<T>(L.xc), D, L.Dp, at<float>(L.zs), flags(), cot,
+               cot.lse ? at<float4>(L.coef) : nullptr);
         return REV_OK;
     }
-    // piece k: first entry, entries, width (a multiple of 8), its rows of W
-    struct Piece { int v0, n, width; const T* w; };
+    int join(const RowResults& out, bool three) {
+        ProfScope ps(K_REDUCE, s, 12.0 * L.Mp * L.strips);
+        if (three) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
+        else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
+        return REV_OK;
+    }
+
+    // ---- bf16 ----
+    int gemm_args(VocabGemm* g) {
+        *g = {};
+        g->plan = v.plan; g->x = at<bf16>(L.xc); g->w = g->wp = params; g->bias = bias();
+        g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
+        g->Mp = L.Mp; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
+        if (L.Dp != D) {
+            ProfScope ps(K_CONVERT, s, 2.0 * V * (D + L.Dp));
+            const int64_t chunks = (int64_t)V * L.Dp / 8;
+            LAUNCH(pad_rows_kernel, blocks_of(chunks, 256), dim3(256), params, D, L.Dp, chunks, at<bf16>(L.w));
+            g->wp = at<bf16>(L.w);
+        }
+        return REV_OK;
+    }
+    int forward_bf16(const RowResults& out) {
+        VocabGemm g;
+        RC(gemm_args(&g));
+        RC(vocab_logits(s, g, false, dual(), L.Mp / 256 * ((V + 255) / 256)));
+        return join(out, dual());
+    }
+    int backward_bf16(void* dX, void* dparams) {
+        VocabGemm g;
+        RC(gemm_args(&g));
+        for (int k = 0; k < L.pieces; ++k) {
+            // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
+            const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
+            g.piece = k;
+            RC(vocab_logits(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
+            LAUNCH(sparse_dz_kernel<bf16>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz), (int64_t)0);
+            if (dX) RC(vocab_dx(s, g, L.lim.slots));
+            if (dparams) RC(vocab_dw(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
+        }
+        return dX ? vocab_dx_rows(s, g, v.place, M, (bf16*)dX) : REV_OK;
+    }
+
+    // ---- float32 ----
+    struct Piece { int v0, n, width; const float* w; };              // first entry, entries, width (a multiple of 4), its rows of W
     int piece(int k, Piece* p) {
         const bool last = L.rest && k == L.pieces - 1;
         p->v0 = last ? V - L.rest : k * L.Vc;
-        p->n = last ? L.rest : std::min(L.Vc, V / 8 * 8 - p->v0);
-        p->width = last ? 8 : p->n;
+        p->n = last ? L.rest : std::min(L.Vc, V / 4 * 4 - p->v0);
+        p->width = last ? 4 : p->n;
         p->w = params + (int64_t)p->v0 * D;
         if (last) {
-            hipLaunchKernelGGL(copy_rows_kernel<T>, blocks_of(8 * D, 256), dim3(256), 0, s, p->w, (int64_t)L.rest * D, (int64_t)8 * D, at<T>(L.w));
-            REV_HIP(hipGetLastError());
-            p->w = at<T>(L.w);
+            LAUNCH(copy_kernel, blocks_of(4 * D, 256), dim3(256), p->w, L.rest * D, 4 * D, at<float>(L.w));
+            p->w = at<float>(L.w);
         }
-        return REV_OK;
+        Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = at<float>(L.dz); e.ldo = p->width; e.solo = true;
+        return gemm_nt_f32(s, at<float>(L.xc), D, p->w, D, (int)L.Mp, p->width, D, e);
     }
-    int logits(const Piece& p) {
-        Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = at<float>(L.z); e.ldo = p.width; e.solo = true;
-        if constexpr (kBf16) return gemm_nt_bf16(s, at<T>(L.xc), L.Dp, p.w, D, (int)L.Mp, p.width, D, e);
-        else return gemm_nt_f32(s, at<T>(L.xc), L.Dp, p.w, D, (int)L.Mp, p.width, D, e);
-    }
-
-    int forward(const void* X, float* loss_ce, float* loss_kd, float* lse) {
-        RC(prepare(X));
+    int forward_f32(const RowResults& out) {
         for (int k = 0; k < L.pieces; ++k) {
             Piece p;
             RC(piece(k, &p));
-            RC(logits(p));
-            hipLaunchKernelGGL(piece_stats_kernel<T>, dim3(M), dim3(256), 0, s, at<float>(L.z), (int64_t)p.width, p.n, bias() ? bias() + p.v0 : nullptr,
-                               at<int>(L.count), v.inv_tau, L.Mp, at<float>(L.stats) + (int64_t)k * 3 * L.Mp);
-            REV_HIP(hipGetLastError());
+            LAUNCH(piece_stats_kernel, dim3(M), dim3(256), at<float>(L.dz), (int64_t)p.width, p.n, bias() ? bias() + p.v0 : nullptr, v.plan, v.inv_tau,
+                   L.Mp, at<float>(L.stats) + (int64_t)k * 3 * L.Mp);
         }
-        ProfScope ps(K_REDUCE, s, 12.0 * L.Mp * L.pieces);
-        hipLaunchKernelGGL(losses_kernel, blocks_of(M, 4), dim3(256), 0, s, v, at<float>(L.stats), L.pieces, L.Mp, at<float>(L.zs), loss_ce, loss_kd,
-                           lse, lse + M);
-        REV_HIP(hipGetLastError());
-        return REV_OK;
+        return join(out, true);
     }
-
-    int backward(const void* X, const float* lse, const float* dce, const float* dkd, void* dX, void* dparams) {
-        RC(prepare(X));
-        hipLaunchKernelGGL(coef_kernel, blocks_of(M, 256), dim3(256), 0, s, v, flags(), lse, lse + M, dce, dkd, at<float4>(L.coef));
-        REV_HIP(hipGetLastError());
-        const bool gb = c.grad_mode == REV_MODE_BF16;
+    int backward_f32(float* dX, float* dparams) {
+        float *dz = at<float>(L.dz), *acc = at<float>(L.acc), *more = at<float>(L.more);
         for (int k = 0; k < L.pieces; ++k) {
             Piece p;
             RC(piece(k, &p));
-            RC(logits(p));
-            T* dz = at<T>(L.dz);
-            hipLaunchKernelGGL(piece_dz_kernel<T>, dim3((unsigned)((p.width + 255) / 256 * L.Mp)), dim3(256), 0, s, at<float>(L.z), (int64_t)p.width, p.n,
-                               bias() ? bias() + p.v0 : nullptr, at<int>(L.count), at<float4>(L.coef), v.inv_tau, (int64_t)p.width, dz);
-            REV_HIP(hipGetLastError());
-            hipLaunchKernelGGL(sparse_dz_kernel<T>, blocks_of(M, 4), dim3(256), 0, s, v, at<float>(L.zs), at<float4>(L.coef), p.v0, p.n, dz,
-                               (int64_t)p.width);
-            REV_HIP(hipGetLastError());
+            LAUNCH(piece_dz_kernel, dim3((unsigned)((p.width + 255) / 256 * L.Mp)), dim3(256), dz, (int64_t)p.width, p.n, bias() ? bias() + p.v0 : nullptr,
+                   v.plan, at<float4>(L.coef), v.inv_tau);
+            LAUNCH(sparse_dz_kernel<float>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), p.v0, p.n, dz, (int64_t)p.width);
             if (dX) {
-                Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = at<float>(k ? L.dw : L.acc); e.ldo = D; e.solo = true;
-                if constexpr (kBf16) RC(gemm_nn_bf16(s, dz, p.width, p.w, D, (int)L.Mp, D, p.width, e));
-                else RC(gemm_nn_f32(s, dz, p.width, p.w, D, (int)L.Mp, D, p.width, e));
-                if (k) {
-                    hipLaunchKernelGGL(add_kernel, blocks_of(L.Mp * D, 256), dim3(256), 0, s, at<float>(L.dw), L.Mp * D, at<float>(L.acc));
-                    REV_HIP(hipGetLastError());
-                }
+                Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = k ? more : acc; e.ldo = D; e.solo = true;
+                RC(gemm_nn_f32(s, dz, p.width, p.w, D, (int)L.Mp, D, p.width, e));
+                if (k) LAUNCH(add_kernel, blocks_of(L.Mp * D, 256), dim3(256), more, L.Mp * D, acc);
             }
             if (dparams) {
-                float* dw = at<float>(L.dw);
-                if constexpr (kBf16) {
-                    const WgradItem it = {dz, p.width, at<T>(L.xc), L.Dp, p.width, D, dw, nullptr};
-                    RedSeg segs[RED_MAX_SEGS];
-                    int nseg = 0;
-                    RC(gemm_wgrad_bf16_group(s, &it, 1, (int)L.Mp, at<float>(L.wg), L.wg_elems, segs, &nseg));
-                    RC(reduce_multi(s, segs, nseg));
-                } else {
-                    const WgradF32Item it = {dz, p.width, at<T>(L.xc), L.Dp, p.width, D, dw, nullptr};
-                    RC(gemm_wgrad_f32_group(s, &it, 1, (int)L.Mp));
-                }
-                hipLaunchKernelGGL(store_grad_kernel, blocks_of((int64_t)p.n * D, 256), dim3(256), 0, s, dw, (int64_t)p.n * D, dparams,
-                                   (int64_t)p.v0 * D, gb);
-                REV_HIP(hipGetLastError());
-                if (c.bias) {
-                    hipLaunchKernelGGL(piece_colsum_kernel<T>, blocks_of(p.n, 256), dim3(256), 0, s, dz, (int64_t)p.width, p.n, at<int>(L.count), dparams,
-                                       (int64_t)V * D + p.v0, gb);
-                    REV_HIP(hipGetLastError());
-                }
+                float* dw = dparams + (int64_t)p.v0 * D;
+                const WgradF32Item it = {dz, p.width, at<float>(L.xc), D, p.width, D, p.width == p.n ? dw : more, nullptr};
+                RC(gemm_wgrad_f32_group(s, &it, 1, (int)L.Mp));
+                if (p.width != p.n) LAUNCH(copy_kernel, blocks_of(p.n * D, 256), dim3(256), more, p.n * D, p.n * D, dw);
+                if (c.bias) LAUNCH(piece_colsum_kernel, blocks_of(p.n, 64), dim3(1024), dz, (int64_t)p.width, p.n, v.plan, dparams + (int64_t)V * D + p.v0);
             }
         }
-        if (dX) {
-            hipLaunchKernelGGL(scatter_dx_kernel<T>, blocks_of((int64_t)M * D / 4, 256), dim3(256), 0, s, at<float>(L.acc), at<int>(L.place), M, D, (T*)dX);
-            REV_HIP(hipGetLastError());
-        }
+        if (dX) LAUNCH(dx_rows_kernel, blocks_of((int64_t)M * D / 4, 256), dim3(256), acc, v.place, M, D, dX);
         return REV_OK;
+    }
+
+    int forward(const void* X, const RowResults& out) {
+        RC(prepare(X, out, Cotangents{}));
+        if constexpr (kBf16) return forward_bf16(out);
+        else return forward_f32(out);
+    }
+    int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
+        RC(prepare(X, RowResults{}, cot));
+        if constexpr (kBf16) return backward_bf16(dX, dparams);
+        else return backward_f32((float*)dX, (float*)dparams);
     }
 };
 
@@ -585,14 +663,16 @@ static int vocab_common(const rev_vocab_cfg* cfg, const void* params, const void
 static int vocab_forward(const rev_vocab_cfg* cfg, const void* params, const void* X, const int* labels, const int* idx, const float* logits,
                          float* loss_ce, float* loss_kd, float* lse, void* ws, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    if (cfg->mode == REV_MODE_BF16) return VocabRunner<bf16>(*cfg, params, ws, s, labels, idx, logits).forward(X, loss_ce, loss_kd, lse);
-    return VocabRunner<float>(*cfg, params, ws, s, labels, idx, logits).forward(X, loss_ce, loss_kd, lse);
+    const RowResults out = {{loss_ce, lse, loss_kd, idx ? lse + cfg->rows : nullptr}};
+    if (cfg->mode == REV_MODE_BF16) return VocabRunner<bf16>(*cfg, params, ws, s, labels, idx, logits).forward(X, out);
+    return VocabRunner<float>(*cfg, params, ws, s, labels, idx, logits).forward(X, out);
 }
 static int vocab_backward(const rev_vocab_cfg* cfg, const void* params, const void* X, const int* labels, const int* idx, const float* logits,
                           const float* lse, const float* dce, const float* dkd, void* dX, void* dparams, void* ws, void* stream) {
     hipStream_t s = (hipStream_t)stream;
-    if (cfg->mode == REV_MODE_BF16) return VocabRunner<bf16>(*cfg, params, ws, s, labels, idx, logits).backward(X, lse, dce, dkd, dX, dparams);
-    return VocabRunner<float>(*cfg, params, ws, s, labels, idx, logits).backward(X, lse, dce, dkd, dX, dparams);
+    const Cotangents cot = {lse, lse + cfg->rows, dce, dkd};
+    if (cfg->mode == REV_MODE_BF16) return VocabRunner<bf16>(*cfg, params, ws, s, labels, idx, logits).backward(X, cot, dX, dparams);
+    return VocabRunner<float>(*cfg, params, ws, s, labels, idx, logits).backward(X, cot, dX, dparams);
 }
 
 int rev_xent_forward(const rev_vocab_cfg* cfg, const void* params, const void* X, const int32_t* labels, float* loss, float* lse,
