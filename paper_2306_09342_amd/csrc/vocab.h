@@ -30,6 +30,8 @@ __device__ __forceinline__ float dense_dz(const float4& c, float z, float inv_ta
     return d;
 }
 
+struct LabelDz { int label; float dz; };         // a row's label, and dz there
+
 constexpr int LOSS_CE = 1, LOSS_KD = 2;
 // The bf16 products (vocab_gemm.hip).
 struct VocabGemm {
@@ -40,6 +42,7 @@ struct VocabGemm {
     const bf16* bias;               // [V] or null
     float* stats;                   // forward: [half tiles][maximum, sum of exp(z - maximum), ...][Mp]; see vocab_logits_kernel
     const float4* coef;             // backward: of every row that counts (dense_dz)
+    const LabelDz* label_dz;        // of every row that counts, where labels alone are named, or null
     bf16* dz;                       // [rows, width] of a piece
     float* acc;                     // dx, 65536 floats per tile and range
     int64_t Mp;

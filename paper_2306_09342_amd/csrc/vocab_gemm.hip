@@ -227,17 +227,50 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
         dma16_sbase(src, vb[h][1], lds + 8192);
     };
     f32x16_t acc[2][2][2];
+    {
+        // four entries at a time; the last few of the vocabulary by themselves
+        u32x2_t q[2][2][4];
+        const bool quads = p.bias && p.V >= 4;
+        const int shift_n = p.V - v0 - 4;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+            for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * (v >> 2) + 4 * t.g + (v & 3);
-                const float b = c >= n ? -INFINITY : p.bias ? to_f(p.bias[v0 + c]) : 0.f;
-                acc[h][0][i][v] = b;
-                acc[h][1][i][v] = b;
-            }
+                for (int k = 0; k < 4; ++k) {
+                    const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * k + 4 * t.g;
+                    q[h][i][k] = u32x2_t{0, 0};
+                    if (quads && c <= shift_n) q[h][i][k] = *reinterpret_cast<const u32x2_t*>(p.bias + v0 + c);
+                }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const unsigned u = q[h][i][k][e >> 1];
+                        const float b = __uint_as_float(e & 1 ? u & 0xFFFF0000u : u << 16);
+                        acc[h][0][i][4 * k + e] = b;
+                    }
+        if (n0 + 256 > n) {                                        // the vocabulary's or the piece's last tile
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * (v >> 2) + 4 * t.g + (v & 3);
+                        if (c >= n) acc[h][0][i][v] = -INFINITY;
+                        else if (p.bias && (c & ~3) > shift_n) acc[h][0][i][v] = to_f(p.bias[v0 + c]);
+                    }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) acc[h][1][i] = acc[h][0][i];
+    }
     tile_products<false, false>(smem, t, issue_a, issue_b, p.Dp >> 6, acc);
 
     if constexpr (!GRAD) {
@@ -315,6 +348,14 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
                     }
                 }
         }
+        if (p.label_dz) {                                          // the labels of this tile, behind its stores
+            const int row = m0 + (int)threadIdx.x;
+            LabelDz y = {-1, 0.f};
+            if (threadIdx.x < 256 && row < pl.count) y = p.label_dz[row];
+            __syncthreads();
+            const int c = y.label - v0;
+            if (y.label >= 0 && c >= n0 && c < n0 + 256 && c < n) p.dz[row * ldz + c] = from_f<bf16>(y.dz);
+        }
     }
 }
 
@@ -391,10 +432,18 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const i
         const int tiles_d = (p.D + 255) >> 8, tiles = (pl.rows >> 8) * tiles_d, tile = (i >> 8) * tiles_d + (d0 >> 8);
         const int h = d0 >> 7 & 1, wm = d0 >> 6 & 1, ib = d0 >> 5 & 1, j = i >> 7 & 1, wn = i >> 5 & 3, fr = i & 31;
         const float* at = p.acc + (int64_t)tile * 65536 + (wn * 2 + wm) * 8192 + (h * 4 + j * 2 + ib) * 1024 + fr * 4;
-        for (int k = 0; k < pl.splits; ++k) {
-            const float* q = at + (int64_t)k * tiles * 65536;
+        for (int k = 0; k < pl.splits; k += 4) {
+            f32x4_t v[4][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) s[e] += *reinterpret_cast<const f32x4_t*>(q + (e >> 1) * 256 + (e & 1) * 128);
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[u][e] = k + u < pl.splits ? *reinterpret_cast<const f32x4_t*>(at + (int64_t)(k + u) * tiles * 65536 + (e >> 1) * 256 + (e & 1) * 128)
+                                                : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) s[e] += v[u][e];
         }
     }
     bf16* out = dX + (int64_t)r * p.D + d0;
@@ -426,13 +475,17 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
         const int c = threadIdx.x & 31, lane_row = threadIdx.x >> 5;
         float s[8] = {};
         const bf16* src = p.dz + b * 256 + c * 8;
-        for (int r = lane_row; r < pl.count; r += 16) {
-            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(src + r * ldz);
+        for (int r0 = lane_row; r0 < pl.count; r0 += 128) {        // eight rows in flight (rows behind the last hold zeros)
+            u32x4_t v[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[2 * e] += __uint_as_float(v[e] << 16);
-                s[2 * e + 1] += __uint_as_float(v[e] & 0xFFFF0000u);
-            }
+            for (int u = 0; u < 8; ++u) v[u] = r0 + 16 * u < pl.rows ? *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz) : u32x4_t{};
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    s[2 * e] += __uint_as_float(v[u][e] << 16);
+                    s[2 * e + 1] += __uint_as_float(v[u][e] & 0xFFFF0000u);
+                }
         }
         float* sh = reinterpret_cast<float*>(smem);
 #pragma unroll

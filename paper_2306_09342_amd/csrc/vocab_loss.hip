@@ -21,19 +21,24 @@ struct PlanLimits { int64_t dz; int tiles_d, slots; };
 struct RowResults { float* p[4]; };
 
 // Pieces of equal widths whose dz fits.  dx has few tiles: its contraction, the piece, is cut into the number of ranges that keeps the
-// 256 CUs busiest; a range costs about 10 stages besides its own (first loads, and writing and reading 256 KB).
-__device__ __forceinline__ VocabPlan plan_of(int count, int V, const PlanLimits& lim) {
+// 256 CUs busiest; a range costs about 10 stages besides its own (first loads, and writing and reading 256 KB).  By one wavefront,
+// a number of ranges per lane.
+__device__ __forceinline__ void write_plan(int count, int V, const PlanLimits& lim, VocabPlan* __restrict__ plan, int lane) {
     VocabPlan p = {count, (count + 255) / 256 * 256, (V + 255) / 256 * 256, 1, 2};
-    if (lim.dz == 0 || count == 0) return p;                       // (without rows: one piece of zeros for dW)
-    const int64_t most = lim.dz / p.rows / 256 * 256, pieces = (V + most - 1) / most;
-    p.width = (int)((V + pieces - 1) / pieces + 255) / 256 * 256;
-    const int tiles = p.rows / 256 * lim.tiles_d, pairs = p.width / 128;
-    int64_t best = 1ll << 62;
-    for (int s = 1; s <= 64 && s <= pairs && tiles * s <= lim.slots; ++s) {
-        const int64_t cost = (int64_t)((tiles * s + 255) / 256) * ((pairs + s - 1) / s * 2 + 10);
-        if (cost < best) { best = cost; p.splits = s; p.stages = (pairs + s - 1) / s * 2; }
+    if (lim.dz != 0 && count != 0) {                               // (without rows: one piece of zeros for dW)
+        const unsigned most = (unsigned)((lim.dz / 256) / (p.rows / 256) / 256 * 256), pieces = (V + most - 1) / most;
+        p.width = (int)((V + pieces - 1) / pieces + 255) / 256 * 256;
+        const int tiles = p.rows / 256 * lim.tiles_d, pairs = p.width / 128, s = lane + 1;
+        const int stages = (pairs + s - 1) / s * 2;
+        unsigned cost = s <= pairs && tiles * s <= lim.slots ? (unsigned)((tiles * s + 255) / 256) * (stages + 10) : ~0u;
+        unsigned best = cost;
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) best = min(best, (unsigned)__shfl_xor((int)best, o, 64));
+        const int who = __ffsll((unsigned long long)__ballot(cost == best)) - 1;
+        p.splits = who + 1;
+        p.stages = __shfl(stages, who, 64);
     }
-    return p;
+    if (lane == 0) *plan = p;
 }
 
 // ---------------------------------------------------------------------------------
@@ -65,10 +70,11 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict
     for (int r0 = 0; r0 < M; r0 += 16384) {
         const int first = r0 + tid * 16;
         unsigned mask = 0;
-        for (int k = 0; k < 16; ++k) {
-            const int r = first + k;
-            if (r < M && (flags ? flags[r] != 0 : in_vocab(labels[r], V))) mask |= 1u << k;
-        }
+        int y[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) y[k] = first + k < M ? flags ? flags[first + k] ? 0 : -1 : labels[first + k] : -1;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) mask |= in_vocab(y[k], V) ? 1u << k : 0u;
         int incl = __popc(mask);
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -99,22 +105,7 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict
         base += total;
         __syncthreads();
     }
-    if (tid == 0) *plan = plan_of(base, V, lim);
-}
-
-// Xc[i] = X[list[i]], padded with zeros to Dp columns and to all of Mp rows.  Chunks of 16 bytes, one per thread.
-template <typename T>
-__global__ __launch_bounds__(256) void gather_rows_kernel(const T* __restrict__ X, const int* __restrict__ list, const VocabPlan* __restrict__ plan,
-                                                          int D, int Dp, int64_t chunks, T* __restrict__ Xc) {
-    constexpr int E = 16 / sizeof(T);
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= chunks) return;
-    const int per = Dp / E;
-    const int64_t i = c / per;
-    const int d = (int)(c - i * per) * E;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (i < plan->count && d < D) v = *reinterpret_cast<const uint4*>(X + (int64_t)list[i] * D + d);
-    *reinterpret_cast<uint4*>(Xc + i * Dp + d) = v;
+    if (tid < 64) write_plan(base, V, lim, plan, tid);
 }
 
 // The rows of W, padded with zeros to Dp columns (a multiple of 128, which the bf16 product over them needs).
@@ -141,25 +132,35 @@ __device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
     return teacher_counts(v.idx[at], v.logits[at], v.V) ? v.idx[at] : -1;
 }
 
-// zs[i][e] = <W_v, x> + b_v.  One workgroup per row, one wavefront per entry at a time.  Bound by reading the rows of W,
-// scattered over all of it.  In the backward pass also what the row's dense part is made of.
+// Row i of Xc = X[list[i]], padded with zeros to Dp columns and to whole tiles of rows, and zs[i][e] = <W_v, x> + b_v for its entries: one
+// workgroup per row, one wavefront per entry at a time.  Bound by reading the rows of W, scattered over all of it: 64 entries of 8192
+// rows of 1024, 1.07 GB, in 160 us.  In the backward pass also what the row's dense part is made of, and dz at its label, which
+// without a teacher is all that is named.
 struct Cotangents { const float *lse, *lse_tau, *dce, *dkd; };
 template <typename T>
-__global__ __launch_bounds__(256) void sparse_logits_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ Xc, int D, int Dp,
-                                                            float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
-                                                            float4* __restrict__ coef) {
+__global__ __launch_bounds__(256) void gather_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ X, int D, int Dp, T* __restrict__ Xc,
+                                                     float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
+                                                     float4* __restrict__ coef, LabelDz* __restrict__ label_dz) {
     constexpr int E = 16 / sizeof(T);
-    const int i = blockIdx.x;
-    if (i >= v.plan->count) return;
-    const int lane = threadIdx.x & 63, r = v.list[i];
-    if (coef && threadIdx.x == 0) {
+    const int i = blockIdx.x, count = v.plan->count;
+    if (sizeof(T) == 2 && i >= v.plan->rows) return;               // (the float32 products go over all rows)
+    T* xc = Xc + (int64_t)i * Dp;
+    const int r = i < count ? v.list[i] : 0;
+    const T* x = X + (int64_t)r * D;
+    for (int d = threadIdx.x * E; d < Dp; d += 256 * E) {
+        uint4 u = make_uint4(0, 0, 0, 0);
+        if (i < count && d < D) u = *reinterpret_cast<const uint4*>(x + d);
+        *reinterpret_cast<uint4*>(xc + d) = u;
+    }
+    if (i >= count) return;
+    float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
+    if (coef) {
         const int f = flags ? flags[r] : HAS_LABEL;
-        float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
         if (f & HAS_LABEL) { c.x = cot.dce[r]; c.y = cot.lse[r]; }
         if (f & HAS_TEACHER) { c.z = cot.dkd[r] / v.inv_tau; c.w = cot.lse_tau[r]; }
-        coef[i] = c;
+        if (threadIdx.x == 0) coef[i] = c;
     }
-    const T* x = Xc + (int64_t)i * Dp;
+    const int lane = threadIdx.x & 63;
     for (int e = threadIdx.x >> 6; e <= v.K; e += 4) {
         const int n = entry_of(v, r, e);
         float s = 0.f;
@@ -174,7 +175,9 @@ __global__ __launch_bounds__(256) void sparse_logits_kernel(VocabRows v, const T
             }
         }
         s = wave_sum(s);
-        if (lane == 0) zs[(int64_t)i * (v.K + 1) + e] = n >= 0 && v.bias ? s + to_f(params[(int64_t)v.V * D + n]) : s;
+        if (n >= 0 && v.bias) s += to_f(params[(int64_t)v.V * D + n]);
+        if (lane == 0) zs[(int64_t)i * (v.K + 1) + e] = s;
+        if (e == 0 && lane == 0 && label_dz) label_dz[i] = {n, dense_dz(c, s, v.inv_tau) - c.x};
     }
 }
 
@@ -435,7 +438,7 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // dz of a piece: 256 MB, what the memory-side cache holds, or 256 entries of all rows if that is more
 constexpr int64_t VOCAB_DZ_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, zs, stats, xc, w, dz, acc, more, total;
+    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, more, total;
     int64_t Mp;
     int Dp, strips, pieces;          // bf16: most pieces that a plan may have
     int Vc, rest;                    // float32: width of a piece, entries left over behind whole multiples of 4 (the last piece)
@@ -451,6 +454,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.flags = take(M);
     L.place = take(4 * M);
     L.list = take(4 * M);
+    L.label_dz = take(8 * M);
     L.zs = take(4 * M * (c.top_k + 1));
     if (wide) {
         L.Mp = up(M, 256);
@@ -518,10 +522,8 @@ struct VocabRunner {
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
         if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
         LAUNCH(select_rows_kernel, dim3(1), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
-        const int64_t chunks = L.Mp * L.Dp * sizeof(T) / 16;
-        LAUNCH(gather_rows_kernel<T>, blocks_of(chunks, 256), dim3(256), (const T*)X, at<int>(L.list), v.plan, D, L.Dp, chunks, at<T>(L.xc));
-        LAUNCH(sparse_logits_kernel<T>, dim3(M), dim3(256), v, params, at<T>(L.xc), D, L.Dp, at<float>(L.zs), flags(), cot,
-               cot.lse ? at<float4>(L.coef) : nullptr);
+        LAUNCH(gather_kernel<T>, dim3((unsigned)L.Mp), dim3(256), v, params, (const T*)X, D, L.Dp, at<T>(L.xc), at<float>(L.zs), flags(), cot,
+               cot.lse ? at<float4>(L.coef) : nullptr, cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr);
         return REV_OK;
     }
     int join(const RowResults& out, bool three) {
@@ -535,7 +537,7 @@ struct VocabRunner {
     int gemm_args(VocabGemm* g) {
         *g = {};
         g->plan = v.plan; g->x = at<bf16>(L.xc); g->w = g->wp = params; g->bias = bias();
-        g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
+        g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
         g->Mp = L.Mp; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
         if (L.Dp != D) {
             ProfScope ps(K_CONVERT, s, 2.0 * V * (D + L.Dp));
@@ -559,7 +561,7 @@ struct VocabRunner {
             const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
             g.piece = k;
             RC(vocab_logits(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
-            LAUNCH(sparse_dz_kernel<bf16>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz), (int64_t)0);
+            if (v.idx) LAUNCH(sparse_dz_kernel<bf16>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz), (int64_t)0);
             if (dX) RC(vocab_dx(s, g, L.lim.slots));
             if (dparams) RC(vocab_dw(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
         }
