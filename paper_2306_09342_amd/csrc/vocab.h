@@ -33,26 +33,35 @@ __device__ __forceinline__ float dense_dz(const float4& c, float z, float inv_ta
 struct LabelDz { int label; float dz; };         // a row's label, and dz there
 
 constexpr int LOSS_CE = 1, LOSS_KD = 2;
-// The bf16 products (vocab_gemm.hip).
+// The products (vocab_gemm.hip).  bf16 operands are one part; a float32 one is the sum of three bf16 parts (split3).
 struct VocabGemm {
     const VocabPlan* plan;
-    const bf16* x;                  // rows that count, [Mp, Dp], zeros behind them and beyond D
-    const bf16* w;                  // [V, D]
-    const bf16* wp;                 // the same with rows of Dp, zeros beyond D
-    const bf16* bias;               // [V] or null
+    const bf16* x;                  // rows that count, a part [Mp, Dp], zeros behind them and beyond D
+    const bf16* w;                  // W with rows of ldw for dx: as given, or as wp
+    const bf16* wp;                 // W with rows of Dp, zeros beyond D; a part [V, Dp]
+    const void* bias;               // [V] or null, bf16, or float32 with three parts
     float* stats;                   // forward: [half tiles][maximum, sum of exp(z - maximum), ...][Mp]; see vocab_logits_kernel
     const float4* coef;             // backward: of every row that counts (dense_dz)
     const LabelDz* label_dz;        // of every row that counts, where labels alone are named, or null
-    bf16* dz;                       // [rows, width] of a piece
+    bf16* dz;                       // a part [rows, width] of a piece
     float* acc;                     // dx, 65536 floats per tile and range
-    int64_t Mp;
-    int V, D, Dp, piece;            // piece: its number (backward)
+    int64_t Mp, dz_part;            // dz_part: elements from a part of dz to the next
+    int V, D, Dp, ldw, piece;       // piece: its number (backward)
     int losses;                     // whose exponentials without `dual`: LOSS_CE, LOSS_KD or both (tau = 1)
     float inv_tau;
 };
-int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks);
-int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks);
-int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, bf16* dX);
-int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks);
+// x = p[0] + p[1] + p[2] to 2^-25 of |x|; an infinity or NaN is p[0] alone.
+__device__ __forceinline__ void split3(float x, bf16 (&p)[3]) {
+    p[0] = from_f<bf16>(x);
+    const float r = x - to_f(p[0]);
+    const float rest = fabsf(r) < INFINITY ? r : 0.f;
+    p[1] = from_f<bf16>(rest);
+    p[2] = from_f<bf16>(rest - to_f(p[1]));
+}
+// T: bf16 (one part) or float (three)
+template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks);
+template <typename T> int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks);
+template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, T* dX);
+template <typename T> int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks);
 
 }  // namespace rev

@@ -10,6 +10,10 @@
 // next, as soon as everybody has read it, so seven phases of products pass between a request and its use.  A stage is four phases of
 // one quadrant each; the two wavefronts of a SIMD are half a phase apart, so that one multiplies while the other reads.
 //
+// float32 operands come as three bf16 parts each (split3), and the products whose parts' indices add to at most 2 are summed, the small
+// ones first: six times the stages of bf16 operands, and 2^-23 of |x||w| left out.  The float32 matrix cores take sixteen times the cycles
+// of the bf16 ones.
+//
 // The number of rows, and what follows from it (tiles, width of a piece, ranges), is read from the device (VocabPlan): a workgroup
 // that finds no tile ends at once.
 #include "mfma.h"
@@ -21,6 +25,29 @@ namespace rev {
 constexpr int VG_PART = 16384, VG_LDS = 8 * VG_PART;
 template <int V> using vg_int = std::integral_constant<int, V>;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
+
+// The part of each operand that a stage takes, and the stage within it: six products of parts in turn, `stages` of each.
+template <int P> struct Parts {
+    int stages;
+    __device__ __forceinline__ int term(int kt) const {
+        if (P == 1) return 0;
+        return (kt >= stages) + (kt >= 2 * stages) + (kt >= 3 * stages) + (kt >= 4 * stages) + (kt >= 5 * stages);
+    }
+    __device__ __forceinline__ int a(int t) const { return P == 1 ? 0 : (0x118 >> (2 * t)) & 3; }    // 0 2 1 0 1 0
+    __device__ __forceinline__ int b(int t) const { return P == 1 ? 0 : (0x052 >> (2 * t)) & 3; }    // 2 0 1 1 0 0
+    __device__ __forceinline__ int within(int kt, int t) const { return P == 1 ? kt : kt - t * stages; }
+    __device__ __forceinline__ int total() const { return P == 1 ? stages : 6 * stages; }
+};
+// A value of dz, or three parts of it, `part` apart.
+template <int P> __device__ __forceinline__ void store_dz(bf16* at, int64_t part, float v) {
+    if constexpr (P == 1) {
+        *at = from_f<bf16>(v);
+    } else {
+        bf16 q[3];
+        split3(v, q);
+        at[0] = q[0]; at[part] = q[1]; at[2 * part] = q[2];
+    }
+}
 
 struct TileLane {
     int lane, wave, wm, wn, g, fr;
@@ -187,11 +214,32 @@ __device__ __forceinline__ void clear(f32x16_t (&acc)[2][2][2]) {
 
 constexpr float LOG2E = 1.44269504088896341f;
 
+// 16 accumulator registers as bf16 to 32 consecutive entries, 8 at a time: lanes g = 0 and 1 hold entries 0..3 and 4..7 of every
+// eight; exchanged, each has all of one: g = 0 of the first of a pair of eights, g = 1 of the second.  `out`: of lane g's
+// first eight.
+__device__ __forceinline__ void store_eights(bf16* out, const f32x16_t& d, bool low = true, bool high = true) {
+    typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+    unsigned w[4][2];                                              // [v / 4][pair]
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const bf16x2_t b = {(__bf16)d[4 * q + 2 * k], (__bf16)d[4 * q + 2 * k + 1]};
+            w[q][k] = __builtin_bit_cast(unsigned, b);
+        }
+#pragma unroll
+    for (int q = 0; q < 4; q += 2) {
+        const u32x2_t x0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
+        const u32x2_t x1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
+        if (q == 0 ? low : high) *reinterpret_cast<u32x4_t*>(out + 8 * q) = u32x4_t{x0[0], x1[0], x0[1], x1[1]};
+    }
+}
+
 // The logits of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so that neither
 // costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the sums are of
 // exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are kept side by side.
 // What bounds it: see the file's head; the epilogue is 128 exponentials a lane (twice that with DUAL), which nothing overlaps.
-template <bool GRAD, bool DUAL>
+template <bool GRAD, bool DUAL, int P>
 __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const TileLane t;
@@ -215,23 +263,28 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int q = 0; q < 2; ++q) vb[h][q] = (unsigned)(min(h * 128 + q * 64 + t.row_along(), last) * ldb * 2 + t.byte_along());
+    const Parts<P> parts{p.Dp >> 6};
+    const int64_t part_a = p.Mp * lda * 2, part_b = p.V * ldb * 2;
     auto issue_a = [&](auto half, int kt, unsigned lds) {
-        const char* src = a_base + decltype(half)::value * 256 * lda + kt * 128;
+        const int term = parts.term(kt);
+        const char* src = a_base + parts.a(term) * part_a + decltype(half)::value * 256 * lda + parts.within(kt, term) * 128;
         dma16_sbase(src, va, lds);
         dma16_sbase(src + 128 * lda, va, lds + 8192);
     };
     auto issue_b = [&](auto half, int kt, unsigned lds) {
         constexpr int h = decltype(half)::value;
-        const char* src = b_base + kt * 128;
+        const int term = parts.term(kt);
+        const char* src = b_base + parts.b(term) * part_b + parts.within(kt, term) * 128;
         dma16_sbase(src, vb[h][0], lds);
         dma16_sbase(src, vb[h][1], lds + 8192);
     };
     f32x16_t acc[2][2][2];
     {
         // four entries at a time; the last few of the vocabulary by themselves
-        u32x2_t q[2][2][4];
-        const bool quads = p.bias && p.V >= 4;
-        const int shift_n = p.V - v0 - 4;
+        const int quad_end = p.V - v0 - 4;
+        auto bias_at = [&](int c) {
+            return P == 1 ? to_f(reinterpret_cast<const bf16*>(p.bias)[v0 + c]) : reinterpret_cast<const float*>(p.bias)[v0 + c];
+        };
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -239,21 +292,19 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * k + 4 * t.g;
-                    q[h][i][k] = u32x2_t{0, 0};
-                    if (quads && c <= shift_n) q[h][i][k] = *reinterpret_cast<const u32x2_t*>(p.bias + v0 + c);
-                }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const unsigned u = q[h][i][k][e >> 1];
-                        const float b = __uint_as_float(e & 1 ? u & 0xFFFF0000u : u << 16);
-                        acc[h][0][i][4 * k + e] = b;
+                    f32x4_t b = {0.f, 0.f, 0.f, 0.f};
+                    if (p.bias && c <= quad_end) {
+                        if (P == 1) {
+                            const u32x2_t u = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const bf16*>(p.bias) + v0 + c);
+                            b = f32x4_t{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16),
+                                        __uint_as_float(u[1] & 0xFFFF0000u)};
+                        } else {
+                            b = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p.bias) + v0 + c);
+                        }
                     }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[h][0][i][4 * k + e] = b[e];
+                }
         if (n0 + 256 > n) {                                        // the vocabulary's or the piece's last tile
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -263,7 +314,7 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
                     for (int v = 0; v < 16; ++v) {
                         const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * (v >> 2) + 4 * t.g + (v & 3);
                         if (c >= n) acc[h][0][i][v] = -INFINITY;
-                        else if (p.bias && (c & ~3) > shift_n) acc[h][0][i][v] = to_f(p.bias[v0 + c]);
+                        else if (p.bias && (c & ~3) > quad_end) acc[h][0][i][v] = bias_at(c);
                     }
         }
 #pragma unroll
@@ -271,7 +322,7 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) acc[h][1][i] = acc[h][0][i];
     }
-    tile_products<false, false>(smem, t, issue_a, issue_b, p.Dp >> 6, acc);
+    tile_products<false, false>(smem, t, issue_a, issue_b, parts.total(), acc);
 
     if constexpr (!GRAD) {
         const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
@@ -322,29 +373,22 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    unsigned w[4][2];                              // [v / 4][pair]
+                    f32x16_t d;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
+                    for (int v = 0; v < 16; ++v) {
+                        const float z = acc[h][j][i][v];
+                        d[v] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
+                        if (DUAL) d[v] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[v]);
+                    }
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            float d[2];
+                    for (int part = 0; part < P; ++part) {
+                        store_eights(out + part * p.dz_part + h * 128 + i * 32, d);
+                        if (part + 1 < P)
 #pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                const float z = acc[h][j][i][4 * q + 2 * k + u];
-                                d[u] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
-                                if (DUAL) d[u] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[u]);
+                            for (int v = 0; v < 16; ++v) {
+                                const float r = d[v] - to_f(from_f<bf16>(d[v]));
+                                d[v] = fabsf(r) < INFINITY ? r : 0.f;
                             }
-                            typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-                            const bf16x2_t b = {(__bf16)d[0], (__bf16)d[1]};
-                            w[q][k] = __builtin_bit_cast(unsigned, b);
-                        }
-                    // lanes g = 0 and 1 hold entries 0..3 and 4..7 of every eight; exchanged, each has all of one eight: g = 0 of the first of
-                    // a pair of eights, g = 1 of the second
-#pragma unroll
-                    for (int q = 0; q < 4; q += 2) {
-                        const u32x2_t x0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
-                        const u32x2_t x1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
-                        *reinterpret_cast<u32x4_t*>(out + h * 128 + i * 32 + 8 * q) = u32x4_t{x0[0], x1[0], x0[1], x1[1]};
                     }
                 }
         }
@@ -354,13 +398,14 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
             if (threadIdx.x < 256 && row < pl.count) y = p.label_dz[row];
             __syncthreads();
             const int c = y.label - v0;
-            if (y.label >= 0 && c >= n0 && c < n0 + 256 && c < n) p.dz[row * ldz + c] = from_f<bf16>(y.dz);
+            if (y.label >= 0 && c >= n0 && c < n0 + 256 && c < n) store_dz<P>(p.dz + row * ldz + c, p.dz_part, y.dz);
         }
     }
 }
 
 // dx of 256 rows and 256 columns over a range of a piece of the vocabulary, in float32, to a place of the range's own, in the order of
-// the accumulators (dx_of_fragments reads it); later pieces add to it.
+// the accumulators (vocab_dx_rows_kernel reads it); later pieces add to it.
+template <int P>
 __global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const TileLane t;
@@ -376,34 +421,38 @@ __global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
     f32x16_t acc[2][2][2];
     clear(acc);
     if (nst > 0) {
-        const int64_t lda = width, ldb = p.D;
+        const int64_t lda = width, ldb = p.ldw;
         const unsigned va = (unsigned)(t.row_along() * lda * 2 + t.byte_along());
         const char* a_base = reinterpret_cast<const char*>(p.dz + m0 * lda + st0 * 64);
         const char* b_base = reinterpret_cast<const char*>(p.w + (int64_t)v0 * ldb + n0);
-        unsigned col[2];                                           // columns beyond D read the last eight again (never used)
+        unsigned col[2];                                           // columns beyond a row read its last eight again (never used)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) col[h] = (unsigned)min(h * 256 + t.byte_across(), (p.D - 8 - n0) * 2);
+        for (int h = 0; h < 2; ++h) col[h] = (unsigned)min(h * 256 + t.byte_across(), (p.ldw - 8 - n0) * 2);
         const unsigned vrow = (unsigned)(t.row_across() * ldb * 2);
+        const Parts<P> parts{nst};
+        const int64_t part_a = p.dz_part * 2, part_b = p.V * ldb * 2;
         auto issue_a = [&](auto half, int kt, unsigned lds) {
-            const char* src = a_base + decltype(half)::value * 256 * lda + kt * 128;
+            const int term = parts.term(kt);
+            const char* src = a_base + parts.a(term) * part_a + decltype(half)::value * 256 * lda + parts.within(kt, term) * 128;
             dma16_sbase(src, va, lds);
             dma16_sbase(src + 128 * lda, va, lds + 8192);
         };
         auto issue_b = [&](auto half, int kt, unsigned lds) {
             constexpr int h = decltype(half)::value;
-            const int k0 = (st0 + kt) * 64;
+            const int term = parts.term(kt), k0 = (st0 + parts.within(kt, term)) * 64;
+            const char* of = b_base + parts.b(term) * part_b;
             if (k0 + 64 <= n) {
-                const char* src = b_base + k0 * ldb * 2;
+                const char* src = of + k0 * ldb * 2;
                 dma16_sbase(src, vrow + col[h], lds);
                 dma16_sbase(src + 64 * ldb, vrow + col[h], lds + 8192);
             } else {                                               // rows beyond the piece, where dz is 0, read its last one
                 const int first = min(k0, n - 1), left = n - 1 - first;
-                const char* src = b_base + first * ldb * 2;
+                const char* src = of + first * ldb * 2;
                 dma16_sbase(src, (unsigned)(min(t.row_across(), left) * ldb * 2) + col[h], lds);
                 dma16_sbase(src, (unsigned)(min(t.row_across() + 32, left) * ldb * 2) + col[h], lds + 8192);
             }
         };
-        tile_products<false, true>(smem, t, issue_a, issue_b, nst, acc);
+        tile_products<false, true>(smem, t, issue_a, issue_b, parts.total(), acc);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -422,7 +471,8 @@ __global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
 }
 
 // dX[r], 32 columns per thread: the ranges' sums of the row's place added in order; zeros for a row that does not count.
-__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const int* __restrict__ place, int M, bf16* __restrict__ dX) {
+template <typename T>
+__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const int* __restrict__ place, int M, T* __restrict__ dX) {
     const int blocks = (p.D + 31) >> 5, r = blockIdx.x * 64 + (threadIdx.x & 63), cb = blockIdx.y * 4 + (threadIdx.x >> 6);
     if (r >= M || cb >= blocks) return;
     const int i = place[r], d0 = cb * 32;
@@ -446,21 +496,26 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const i
                 for (int e = 0; e < 8; ++e) s[e] += v[u][e];
         }
     }
-    bf16* out = dX + (int64_t)r * p.D + d0;
+    T* out = dX + (int64_t)r * p.D + d0;
 #pragma unroll
     for (int e = 0; e < 8; e += 2)
         if (d0 + e * 4 < p.D) {
-            typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-            bf16x8 b;
+            if constexpr (sizeof(T) == 2) {
+                typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+                bf16x8 b;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) { b[k] = (__bf16)s[e][k]; b[4 + k] = (__bf16)s[e + 1][k]; }
-            *reinterpret_cast<bf16x8*>(out + e * 4) = b;
+                for (int k = 0; k < 4; ++k) { b[k] = (__bf16)s[e][k]; b[4 + k] = (__bf16)s[e + 1][k]; }
+                *reinterpret_cast<bf16x8*>(out + e * 4) = b;
+            } else {
+                *reinterpret_cast<f32x4_t*>(out + e * 4) = s[e];
+                *reinterpret_cast<f32x4_t*>(out + e * 4 + 4) = s[e + 1];
+            }
         }
 }
 
 // dW of 256 entries of a piece and 256 columns over all rows, and, in the workgroups behind the tiles, db of 256 entries each: these
 // find the CUs that the last round of tiles leaves idle.
-template <typename TG>
+template <typename TG, int P>
 __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dparams, int db) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     const TileLane t;
@@ -474,18 +529,21 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
         if (!db || b >= tiles_v) return;
         const int c = threadIdx.x & 31, lane_row = threadIdx.x >> 5;
         float s[8] = {};
-        const bf16* src = p.dz + b * 256 + c * 8;
-        for (int r0 = lane_row; r0 < pl.count; r0 += 128) {        // eight rows in flight (rows behind the last hold zeros)
-            u32x4_t v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = r0 + 16 * u < pl.rows ? *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz) : u32x4_t{};
+        for (int part = P - 1; part >= 0; --part) {
+            const bf16* src = p.dz + part * p.dz_part + b * 256 + c * 8;
+            for (int r0 = lane_row; r0 < pl.count; r0 += 128) {    // eight rows in flight (rows behind the last hold zeros)
+                u32x4_t v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u)
+                for (int u = 0; u < 8; ++u) v[u] = r0 + 16 * u < pl.rows ? *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz) : u32x4_t{};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[2 * e] += __uint_as_float(v[u][e] << 16);
-                    s[2 * e + 1] += __uint_as_float(v[u][e] & 0xFFFF0000u);
-                }
+                for (int u = 0; u < 8; ++u)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        s[2 * e] += __uint_as_float(v[u][e] << 16);
+                        s[2 * e + 1] += __uint_as_float(v[u][e] & 0xFFFF0000u);
+                    }
+            }
         }
         float* sh = reinterpret_cast<float*>(smem);
 #pragma unroll
@@ -512,17 +570,21 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
         for (int h = 0; h < 2; ++h) vb[h] = (unsigned)(t.row_across() * ldb * 2 + min(h * 256 + t.byte_across(), (p.Dp - 8 - n0) * 2));
         const char* a_base = reinterpret_cast<const char*>(p.dz + m0);
         const char* b_base = reinterpret_cast<const char*>(p.x + n0);
+        const Parts<P> parts{nst};
+        const int64_t part_a = p.dz_part * 2, part_b = p.Mp * ldb * 2;
         auto issue_a = [&](auto half, int kt, unsigned lds) {
-            const char* src = a_base + decltype(half)::value * 256 + kt * 128 * ldz;
+            const int term = parts.term(kt);
+            const char* src = a_base + parts.a(term) * part_a + decltype(half)::value * 256 + parts.within(kt, term) * 128 * ldz;
             dma16_sbase(src, va, lds);
             dma16_sbase(src + 64 * ldz, va, lds + 8192);
         };
         auto issue_b = [&](auto half, int kt, unsigned lds) {
-            const char* src = b_base + kt * 128 * ldb;
+            const int term = parts.term(kt);
+            const char* src = b_base + parts.b(term) * part_b + parts.within(kt, term) * 128 * ldb;
             dma16_sbase(src, vb[decltype(half)::value], lds);
             dma16_sbase(src + 64 * ldb, vb[decltype(half)::value], lds + 8192);
         };
-        tile_products<true, true>(smem, t, issue_a, issue_b, nst, acc);
+        tile_products<true, true>(smem, t, issue_a, issue_b, parts.total(), acc);
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -546,22 +608,8 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    unsigned w[4][2];
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
-                            const bf16x2_t b = {(__bf16)acc[h][j][i][4 * q + 2 * k], (__bf16)acc[h][j][i][4 * q + 2 * k + 1]};
-                            w[q][k] = __builtin_bit_cast(unsigned, b);
-                        }
-#pragma unroll
-                    for (int q = 0; q < 4; q += 2) {
-                        const u32x2_t x0 = __builtin_amdgcn_permlane32_swap(w[q][0], w[q + 1][0], false, false);
-                        const u32x2_t x1 = __builtin_amdgcn_permlane32_swap(w[q][1], w[q + 1][1], false, false);
-                        const int d = h * 128 + i * 32 + 8 * q + 8 * t.g;
-                        if (v < n && n0 + t.wm * 64 + d < p.D) *reinterpret_cast<u32x4_t*>(out + d) = u32x4_t{x0[0], x1[0], x0[1], x1[1]};
-                    }
+                    const int d = n0 + t.wm * 64 + h * 128 + i * 32 + 8 * t.g;
+                    store_eights(out + h * 128 + i * 32 + 8 * t.g, acc[h][j][i], v < n && d < p.D, v < n && d + 16 < p.D);
                 }
         }
     }
@@ -575,28 +623,44 @@ static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipSt
     return REV_OK;
 }
 
+template <typename T> constexpr int parts_of = sizeof(T) == 2 ? 1 : 3;
+
+template <typename T>
 int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks) {
+    constexpr int P = parts_of<T>;
     ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
     static LdsLimit lim[4];
-    if (grad) return dual ? launch_tiles(vocab_logits_kernel<true, true>, lim[0], blocks, s, p) : launch_tiles(vocab_logits_kernel<true, false>, lim[1], blocks, s, p);
-    return dual ? launch_tiles(vocab_logits_kernel<false, true>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false>, lim[3], blocks, s, p);
+    if (grad) return dual ? launch_tiles(vocab_logits_kernel<true, true, P>, lim[0], blocks, s, p) : launch_tiles(vocab_logits_kernel<true, false, P>, lim[1], blocks, s, p);
+    return dual ? launch_tiles(vocab_logits_kernel<false, true, P>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false, P>, lim[3], blocks, s, p);
 }
+template <typename T>
 int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks) {
     ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
     static LdsLimit lim;
-    return launch_tiles(vocab_dx_kernel, lim, blocks, s, p);
+    return launch_tiles(vocab_dx_kernel<parts_of<T>>, lim, blocks, s, p);
 }
-int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, bf16* dX) {
-    ProfScope ps(K_REDUCE, s, 6.0 * M * p.D);
-    hipLaunchKernelGGL(vocab_dx_rows_kernel, dim3((M + 63) / 64, ((p.D + 31) / 32 + 3) / 4), dim3(256), 0, s, p, place, M, dX);
+template <typename T>
+int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, T* dX) {
+    ProfScope ps(K_REDUCE, s, (4.0 + sizeof(T)) * M * p.D);
+    hipLaunchKernelGGL(vocab_dx_rows_kernel<T>, dim3((M + 63) / 64, ((p.D + 31) / 32 + 3) / 4), dim3(256), 0, s, p, place, M, dX);
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
+template <typename T>
 int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks) {
     ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
     static LdsLimit lim[2];
-    if (grad_bf16) return launch_tiles(vocab_dw_kernel<bf16>, lim[0], blocks, s, p, (bf16*)dparams, (int)db);
-    return launch_tiles(vocab_dw_kernel<float>, lim[1], blocks, s, p, (float*)dparams, (int)db);
+    if constexpr (sizeof(T) == 2)
+        if (grad_bf16) return launch_tiles(vocab_dw_kernel<bf16, 1>, lim[0], blocks, s, p, (bf16*)dparams, (int)db);
+    return launch_tiles(vocab_dw_kernel<float, parts_of<T>>, lim[1], blocks, s, p, (float*)dparams, (int)db);
 }
+#define BOTH(T)                                                                                   \
+    template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, int64_t);             \
+    template int vocab_dx<T>(hipStream_t, const VocabGemm&, int64_t);                             \
+    template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, int, T*);            \
+    template int vocab_dw<T>(hipStream_t, const VocabGemm&, void*, bool, bool, int64_t);
+BOTH(bf16)
+BOTH(float)
+#undef BOTH
 
 }  // namespace rev

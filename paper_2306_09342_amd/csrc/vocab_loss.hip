@@ -108,15 +108,33 @@ __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict
     if (tid < 64) write_plan(base, V, lim, plan, tid);
 }
 
-// The rows of W, padded with zeros to Dp columns (a multiple of 128, which the bf16 product over them needs).
-__global__ __launch_bounds__(256) void pad_rows_kernel(const bf16* __restrict__ w, int D, int Dp, int64_t chunks, bf16* __restrict__ out) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= chunks) return;
-    const int64_t i = c / (Dp / 8);
-    const int d = (int)(c - i * (Dp / 8)) * 8;
-    uint4 v = make_uint4(0, 0, 0, 0);
-    if (d < D) v = *reinterpret_cast<const uint4*>(w + i * D + d);
-    *reinterpret_cast<uint4*>(out + i * Dp + d) = v;
+// Four float32 values as three bf16 parts each, `part` elements apart.
+__device__ __forceinline__ void store_parts(uint4 u, bf16* out, int64_t part) {
+    const unsigned x[4] = {u.x, u.y, u.z, u.w};
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    u16x4 q[3];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        bf16 p[3];
+        split3(__uint_as_float(x[e]), p);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) q[k][e] = *reinterpret_cast<const uint16_t*>(&p[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<u16x4*>(out + k * part) = q[k];
+}
+
+// W as the products over its rows take it: padded with zeros to Dp columns, a multiple of 128, float32 in three parts.
+template <typename T>
+__global__ __launch_bounds__(256) void lay_out_kernel(const T* __restrict__ w, int V, int D, int Dp, bf16* __restrict__ out) {
+    constexpr int E = 16 / sizeof(T);
+    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x, i = c / (Dp / E);
+    if (i >= V) return;
+    const int d = (int)(c - i * (Dp / E)) * E;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if (d < D) u = *reinterpret_cast<const uint4*>(w + i * D + d);
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint4*>(out + i * Dp + d) = u;
+    else store_parts(u, out + i * Dp + d, (int64_t)V * Dp);
 }
 
 // ---------------------------------------------------------------------------------
@@ -137,20 +155,21 @@ __device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
 // rows of 1024, 1.07 GB, in 160 us.  In the backward pass also what the row's dense part is made of, and dz at its label, which
 // without a teacher is all that is named.
 struct Cotangents { const float *lse, *lse_tau, *dce, *dkd; };
-template <typename T>
-__global__ __launch_bounds__(256) void gather_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ X, int D, int Dp, T* __restrict__ Xc,
-                                                     float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
+// P: parts that the copy of X has, 0: its own type, over all rows.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void gather_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ X, int D, int Dp, int64_t Mp,
+                                                     void* __restrict__ Xc, float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
                                                      float4* __restrict__ coef, LabelDz* __restrict__ label_dz) {
     constexpr int E = 16 / sizeof(T);
     const int i = blockIdx.x, count = v.plan->count;
-    if (sizeof(T) == 2 && i >= v.plan->rows) return;               // (the float32 products go over all rows)
-    T* xc = Xc + (int64_t)i * Dp;
+    if (P > 0 && i >= v.plan->rows) return;
     const int r = i < count ? v.list[i] : 0;
     const T* x = X + (int64_t)r * D;
     for (int d = threadIdx.x * E; d < Dp; d += 256 * E) {
         uint4 u = make_uint4(0, 0, 0, 0);
         if (i < count && d < D) u = *reinterpret_cast<const uint4*>(x + d);
-        *reinterpret_cast<uint4*>(xc + d) = u;
+        if constexpr (P < 3) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(Xc) + (int64_t)i * Dp + d) = u;
+        else store_parts(u, reinterpret_cast<bf16*>(Xc) + (int64_t)i * Dp + d, Mp * Dp);
     }
     if (i >= count) return;
     float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
@@ -283,9 +302,9 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
 // ---------------------------------------------------------------------------------
 // dz at the entries of a piece that a row names, again.  One wavefront per row; an entry that is named several times is written by
 // the first of them.  The piece: n entries from v0, or with n = 0 number v0 of the plan.
-template <typename T>
+template <typename T, int P>
 __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float* __restrict__ zs, const float4* __restrict__ coef, int v0, int n,
-                                                        T* __restrict__ dz, int64_t ld) {
+                                                        T* __restrict__ dz, int64_t ld, int64_t part) {
     __shared__ int names[4][257];
     __shared__ float probs[4][257];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i = blockIdx.x * 4 + w;
@@ -328,7 +347,16 @@ __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float
                 if (k < e) first = false;
                 less += probs[w][k];
             }
-        if (first) dz[(int64_t)i * ld + name - v0] = from_f<T>(dense_dz(c, zs[(int64_t)i * (v.K + 1) + e], v.inv_tau) - less);
+        if (!first) continue;
+        const float d = dense_dz(c, zs[(int64_t)i * (v.K + 1) + e], v.inv_tau) - less;
+        T* at = dz + (int64_t)i * ld + name - v0;
+        if constexpr (P == 3) {
+            bf16 q[3];
+            split3(d, q);
+            for (int k = 0; k < 3; ++k) at[k * part] = q[k];
+        } else {
+            *at = from_f<T>(d);
+        }
     }
 }
 
@@ -434,19 +462,24 @@ static int vocab_check(const rev_vocab_cfg* c) {
     return REV_OK;
 }
 
+// float32: by parts from PARTS_ROWS rows on
+constexpr int PARTS_ROWS = 128;
+static bool takes_parts(const rev_vocab_cfg& c) { return c.rows > PARTS_ROWS; }
+
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // dz of a piece: 256 MB, what the memory-side cache holds, or 256 entries of all rows if that is more
 constexpr int64_t VOCAB_DZ_BYTES = 256 << 20;
 struct VocabLayout {
     int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, more, total;
     int64_t Mp;
-    int Dp, strips, pieces;          // bf16: most pieces that a plan may have
+    int parts;                       // bf16 parts of an operand of the products; 0: float32 products (gemm_f32.hip)
+    int Dp, strips, pieces;          // parts: most pieces that a plan may have
     int Vc, rest;                    // float32: width of a piece, entries left over behind whole multiples of 4 (the last piece)
     PlanLimits lim;
 };
 static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     VocabLayout L = {};
-    const bool wide = c.mode == REV_MODE_BF16;
+    L.parts = c.mode == REV_MODE_BF16 ? 1 : takes_parts(c) ? 3 : 0;
     const int64_t M = c.rows, D = c.d_model, V = c.vocab;
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
@@ -456,10 +489,10 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.list = take(4 * M);
     L.label_dz = take(8 * M);
     L.zs = take(4 * M * (c.top_k + 1));
-    if (wide) {
+    if (L.parts) {
         L.Mp = up(M, 256);
         L.Dp = (int)up(D, 128);
-        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2, L.Mp * 256), L.Mp * up(V, 256));
+        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), L.Mp * up(V, 256));
         L.lim.tiles_d = (int)((D + 255) / 256);
         L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
@@ -467,9 +500,9 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
         L.strips = (int)((V + 255) / 256) * 2;
         L.coef = take(16 * M);
         L.stats = take(12 * L.Mp * L.strips);
-        L.xc = take(2 * L.Mp * L.Dp);
-        L.w = L.Dp != D ? take(2 * V * L.Dp) : 0;
-        L.dz = take(2 * L.lim.dz);
+        L.xc = take(2 * L.parts * L.Mp * L.Dp);
+        L.w = L.Dp != D || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
+        L.dz = take(2 * L.parts * L.lim.dz);
         L.acc = take((int64_t)L.lim.slots * 65536 * 4);
     } else {
         L.Mp = up(M, 64);
@@ -496,7 +529,7 @@ static dim3 blocks_of(int64_t n, int per) { return dim3((unsigned)((n + per - 1)
 
 template <typename T>
 struct VocabRunner {
-    static constexpr bool kBf16 = sizeof(T) == 2;
+    static constexpr int kParts = sizeof(T) == 2 ? 1 : 3;
     rev_vocab_cfg c;
     VocabLayout L;
     char* ws;
@@ -511,7 +544,7 @@ struct VocabRunner {
         v = {labels, idx, logits, at<int>(L.list), at<int>(L.place), at<VocabPlan>(L.plan), M, V, idx ? c.top_k : 0, c.bias,
              idx ? 1.f / c.temperature : 1.f};
     }
-    template <typename U> U* at(int64_t off) const { return reinterpret_cast<U*>(ws + off); }
+    template <typename U> U* at(int64_t off) const { return static_cast<U*>(static_cast<void*>(ws + off)); }
     const uint8_t* flags() const { return v.idx ? at<uint8_t>(L.flags) : nullptr; }
     const T* bias() const { return c.bias ? params + (int64_t)V * D : nullptr; }
     int losses() const { return (v.labels ? LOSS_CE : 0) | (v.idx ? LOSS_KD : 0); }
@@ -522,8 +555,13 @@ struct VocabRunner {
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
         if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
         LAUNCH(select_rows_kernel, dim3(1), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
-        LAUNCH(gather_kernel<T>, dim3((unsigned)L.Mp), dim3(256), v, params, (const T*)X, D, L.Dp, at<T>(L.xc), at<float>(L.zs), flags(), cot,
-               cot.lse ? at<float4>(L.coef) : nullptr, cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr);
+        float4* coef = cot.lse ? at<float4>(L.coef) : nullptr;
+        LabelDz* label_dz = cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr;
+        const dim3 grid((unsigned)L.Mp), block(256);
+        if (L.parts)
+            LAUNCH((gather_kernel<T, kParts>), grid, block, v, params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), flags(), cot, coef, label_dz);
+        else
+            LAUNCH((gather_kernel<T, 0>), grid, block, v, params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), flags(), cot, coef, label_dz);
         return REV_OK;
     }
     int join(const RowResults& out, bool three) {
@@ -533,49 +571,52 @@ struct VocabRunner {
         return REV_OK;
     }
 
-    // ---- bf16 ----
+    // ---- products of bf16 parts ----
     int gemm_args(VocabGemm* g) {
         *g = {};
-        g->plan = v.plan; g->x = at<bf16>(L.xc); g->w = g->wp = params; g->bias = bias();
-        g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
-        g->Mp = L.Mp; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
-        if (L.Dp != D) {
-            ProfScope ps(K_CONVERT, s, 2.0 * V * (D + L.Dp));
-            const int64_t chunks = (int64_t)V * L.Dp / 8;
-            LAUNCH(pad_rows_kernel, blocks_of(chunks, 256), dim3(256), params, D, L.Dp, chunks, at<bf16>(L.w));
+        g->plan = v.plan; g->x = at<bf16>(L.xc); g->bias = bias(); g->label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz);
+        g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
+        g->Mp = L.Mp; g->dz_part = L.lim.dz; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
+        g->w = g->wp = (const bf16*)params;
+        g->ldw = D;
+        if (L.w) {
+            ProfScope ps(K_CONVERT, s, (sizeof(T) + 2.0 * kParts) * V * L.Dp);
+            LAUNCH(lay_out_kernel<T>, blocks_of((int64_t)V * L.Dp * sizeof(T) / 16, 256), dim3(256), params, V, D, L.Dp, at<bf16>(L.w));
             g->wp = at<bf16>(L.w);
+            if (kParts > 1) { g->w = g->wp; g->ldw = L.Dp; }
         }
         return REV_OK;
     }
-    int forward_bf16(const RowResults& out) {
+    int forward_parts(const RowResults& out) {
         VocabGemm g;
         RC(gemm_args(&g));
-        RC(vocab_logits(s, g, false, dual(), L.Mp / 256 * ((V + 255) / 256)));
+        RC(vocab_logits<T>(s, g, false, dual(), L.Mp / 256 * ((V + 255) / 256)));
         return join(out, dual());
     }
-    int backward_bf16(void* dX, void* dparams) {
+    int backward_parts(T* dX, void* dparams) {
         VocabGemm g;
         RC(gemm_args(&g));
         for (int k = 0; k < L.pieces; ++k) {
             // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
             const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
             g.piece = k;
-            RC(vocab_logits(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
-            if (v.idx) LAUNCH(sparse_dz_kernel<bf16>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz), (int64_t)0);
-            if (dX) RC(vocab_dx(s, g, L.lim.slots));
-            if (dparams) RC(vocab_dw(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
+            RC(vocab_logits<T>(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
+            if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
+                              (int64_t)0, L.lim.dz);
+            if (dX) RC(vocab_dx<T>(s, g, L.lim.slots));
+            if (dparams) RC(vocab_dw<T>(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
         }
-        return dX ? vocab_dx_rows(s, g, v.place, M, (bf16*)dX) : REV_OK;
+        return dX ? vocab_dx_rows<T>(s, g, v.place, M, dX) : REV_OK;
     }
 
-    // ---- float32 ----
+    // ---- float32 products ----
     struct Piece { int v0, n, width; const float* w; };              // first entry, entries, width (a multiple of 4), its rows of W
     int piece(int k, Piece* p) {
         const bool last = L.rest && k == L.pieces - 1;
         p->v0 = last ? V - L.rest : k * L.Vc;
         p->n = last ? L.rest : std::min(L.Vc, V / 4 * 4 - p->v0);
         p->width = last ? 4 : p->n;
-        p->w = params + (int64_t)p->v0 * D;
+        p->w = (const float*)params + (int64_t)p->v0 * D;
         if (last) {
             LAUNCH(copy_kernel, blocks_of(4 * D, 256), dim3(256), p->w, L.rest * D, 4 * D, at<float>(L.w));
             p->w = at<float>(L.w);
@@ -587,7 +628,7 @@ struct VocabRunner {
         for (int k = 0; k < L.pieces; ++k) {
             Piece p;
             RC(piece(k, &p));
-            LAUNCH(piece_stats_kernel, dim3(M), dim3(256), at<float>(L.dz), (int64_t)p.width, p.n, bias() ? bias() + p.v0 : nullptr, v.plan, v.inv_tau,
+            LAUNCH(piece_stats_kernel, dim3(M), dim3(256), at<float>(L.dz), (int64_t)p.width, p.n, bias() ? (const float*)bias() + p.v0 : nullptr, v.plan, v.inv_tau,
                    L.Mp, at<float>(L.stats) + (int64_t)k * 3 * L.Mp);
         }
         return join(out, true);
@@ -597,9 +638,9 @@ struct VocabRunner {
         for (int k = 0; k < L.pieces; ++k) {
             Piece p;
             RC(piece(k, &p));
-            LAUNCH(piece_dz_kernel, dim3((unsigned)((p.width + 255) / 256 * L.Mp)), dim3(256), dz, (int64_t)p.width, p.n, bias() ? bias() + p.v0 : nullptr,
+            LAUNCH(piece_dz_kernel, dim3((unsigned)((p.width + 255) / 256 * L.Mp)), dim3(256), dz, (int64_t)p.width, p.n, bias() ? (const float*)bias() + p.v0 : nullptr,
                    v.plan, at<float4>(L.coef), v.inv_tau);
-            LAUNCH(sparse_dz_kernel<float>, blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), p.v0, p.n, dz, (int64_t)p.width);
+            LAUNCH((sparse_dz_kernel<float, 1>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), p.v0, p.n, dz, (int64_t)p.width, (int64_t)0);
             if (dX) {
                 Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = k ? more : acc; e.ldo = D; e.solo = true;
                 RC(gemm_nn_f32(s, dz, p.width, p.w, D, (int)L.Mp, D, p.width, e));
@@ -619,13 +660,15 @@ struct VocabRunner {
 
     int forward(const void* X, const RowResults& out) {
         RC(prepare(X, out, Cotangents{}));
-        if constexpr (kBf16) return forward_bf16(out);
-        else return forward_f32(out);
+        if (L.parts) return forward_parts(out);
+        if constexpr (kParts == 3) return forward_f32(out);
+        return REV_OK;
     }
     int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
         RC(prepare(X, RowResults{}, cot));
-        if constexpr (kBf16) return backward_bf16(dX, dparams);
-        else return backward_f32((float*)dX, (float*)dparams);
+        if (L.parts) return backward_parts((T*)dX, dparams);
+        if constexpr (kParts == 3) return backward_f32((float*)dX, (float*)dparams);
+        return REV_OK;
     }
 };
 
