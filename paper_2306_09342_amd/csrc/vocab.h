@@ -64,4 +64,21 @@ template <typename T> int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t bl
 template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, T* dX);
 template <typename T> int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks);
 
+// Logits of few rows (vocab_few.hip): their statistics, or dz of the whole vocabulary.
+template <typename T> struct FewRows {
+    const VocabPlan* plan;
+    const T* x;                     // rows that count, [rows_x, Dp]
+    const T* w;                     // [V, D]
+    const T* bias;                  // [V] or null
+    float* stats;                   // as VocabGemm::stats, of strips of 64 entries: row i at i stat_row, kinds stat_kind apart
+    const float4* coef;
+    const LabelDz* label_dz;
+    T* dz;                          // [rows_out, ldz], zeros behind the rows that count and the vocabulary; ldz = 0: the plan's width
+    int64_t stat_row, stat_kind, ldz;
+    int V, D, Dp, losses, rows_x, rows_out, blocks_m;
+    float inv_tau;
+};
+// rows: most that count; width: columns that the launch covers
+template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual, int rows, int64_t width);
+
 }  // namespace rev

@@ -150,42 +150,44 @@ __device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
     return teacher_counts(v.idx[at], v.logits[at], v.V) ? v.idx[at] : -1;
 }
 
-// Row i of Xc = X[list[i]], padded with zeros to Dp columns and to whole tiles of rows, and zs[i][e] = <W_v, x> + b_v for its entries: one
-// workgroup per row, one wavefront per entry at a time.  Bound by reading the rows of W, scattered over all of it: 64 entries of 8192
-// rows of 1024, 1.07 GB, in 160 us.  In the backward pass also what the row's dense part is made of, and dz at its label, which
-// without a teacher is all that is named.
+// Row i of Xc = row r of X, padded with zeros to Dp columns, all zeros beyond the last row that counts; zs[i][e] = <W_v, x> + b_v for its
+// entries, a wavefront of the workgroup per entry at a time; in the backward pass also what the row's dense part is made of, and
+// dz at its label, which without a teacher is all that is named.  P: bf16 parts that the copy has, 0: its own type.
 struct Cotangents { const float *lse, *lse_tau, *dce, *dkd; };
-// P: parts that the copy of X has, 0: its own type, over all rows.
+template <typename T> struct GatherArgs {
+    const T* params; const T* X;
+    int D, Dp;
+    int64_t Mp;
+    void* Xc;
+    float* zs;
+    Cotangents cot;
+    float4* coef;
+    LabelDz* label_dz;
+};
 template <typename T, int P>
-__global__ __launch_bounds__(256) void gather_kernel(VocabRows v, const T* __restrict__ params, const T* __restrict__ X, int D, int Dp, int64_t Mp,
-                                                     void* __restrict__ Xc, float* __restrict__ zs, const uint8_t* __restrict__ flags, Cotangents cot,
-                                                     float4* __restrict__ coef, LabelDz* __restrict__ label_dz) {
+__device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<T>& g, int i, bool live, int r, int flags) {
     constexpr int E = 16 / sizeof(T);
-    const int i = blockIdx.x, count = v.plan->count;
-    if (P > 0 && i >= v.plan->rows) return;
-    const int r = i < count ? v.list[i] : 0;
-    const T* x = X + (int64_t)r * D;
-    for (int d = threadIdx.x * E; d < Dp; d += 256 * E) {
+    const T* x = g.X + (int64_t)r * g.D;
+    for (int d = threadIdx.x * E; d < g.Dp; d += 256 * E) {
         uint4 u = make_uint4(0, 0, 0, 0);
-        if (i < count && d < D) u = *reinterpret_cast<const uint4*>(x + d);
-        if constexpr (P < 3) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(Xc) + (int64_t)i * Dp + d) = u;
-        else store_parts(u, reinterpret_cast<bf16*>(Xc) + (int64_t)i * Dp + d, Mp * Dp);
+        if (live && d < g.D) u = *reinterpret_cast<const uint4*>(x + d);
+        if constexpr (P < 3) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(g.Xc) + (int64_t)i * g.Dp + d) = u;
+        else store_parts(u, reinterpret_cast<bf16*>(g.Xc) + (int64_t)i * g.Dp + d, g.Mp * g.Dp);
     }
-    if (i >= count) return;
+    if (!live) return;
     float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
-    if (coef) {
-        const int f = flags ? flags[r] : HAS_LABEL;
-        if (f & HAS_LABEL) { c.x = cot.dce[r]; c.y = cot.lse[r]; }
-        if (f & HAS_TEACHER) { c.z = cot.dkd[r] / v.inv_tau; c.w = cot.lse_tau[r]; }
-        if (threadIdx.x == 0) coef[i] = c;
+    if (g.coef) {
+        if (flags & HAS_LABEL) { c.x = g.cot.dce[r]; c.y = g.cot.lse[r]; }
+        if (flags & HAS_TEACHER) { c.z = g.cot.dkd[r] / v.inv_tau; c.w = g.cot.lse_tau[r]; }
+        if (threadIdx.x == 0) g.coef[i] = c;
     }
     const int lane = threadIdx.x & 63;
     for (int e = threadIdx.x >> 6; e <= v.K; e += 4) {
         const int n = entry_of(v, r, e);
         float s = 0.f;
         if (n >= 0) {
-            const T* w = params + (int64_t)n * D;
-            for (int d = lane * E; d < D; d += 64 * E) {
+            const T* w = g.params + (int64_t)n * g.D;
+            for (int d = lane * E; d < g.D; d += 64 * E) {
 #pragma unroll
                 for (int q = 0; q < E; q += 4) {
                     const f4 a = load4(x + d + q), b = load4(w + d + q);
@@ -194,10 +196,73 @@ __global__ __launch_bounds__(256) void gather_kernel(VocabRows v, const T* __res
             }
         }
         s = wave_sum(s);
-        if (n >= 0 && v.bias) s += to_f(params[(int64_t)v.V * D + n]);
-        if (lane == 0) zs[(int64_t)i * (v.K + 1) + e] = s;
-        if (e == 0 && lane == 0 && label_dz) label_dz[i] = {n, dense_dz(c, s, v.inv_tau) - c.x};
+        if (n >= 0 && v.bias) s += to_f(g.params[(int64_t)v.V * g.D + n]);
+        if (lane == 0) g.zs[(int64_t)i * (v.K + 1) + e] = s;
+        if (e == 0 && lane == 0 && g.label_dz) g.label_dz[i] = {n, dense_dz(c, s, v.inv_tau) - c.x};
     }
+}
+
+// One workgroup per row of Xc.  Bound by reading the rows of W, scattered over all of it: 64 entries of 8192 rows of 1024, 1.07 GB,
+// in 160 us.
+template <typename T, int P>
+__global__ __launch_bounds__(256) void gather_kernel(VocabRows v, GatherArgs<T> g, const uint8_t* __restrict__ flags) {
+    const int i = blockIdx.x, count = v.plan->count;
+    if (P > 0 && i >= v.plan->rows) return;                        // (the float32 products go over all rows)
+    const int r = i < count ? v.list[i] : 0;
+    gather_row<T, P>(v, g, i, i < count, r, flags ? flags[r] : HAS_LABEL);
+}
+
+// The same for up to SELECT_ROWS rows with up to SELECT_ENTRIES labels and teacher entries, without the launches before it: every
+// workgroup goes over all of them and finds its own row.  The first one leaves what select_rows_kernel does.
+constexpr int SELECT_ROWS = 1024, SELECT_ENTRIES = 8192;
+template <typename T, int P>
+__global__ __launch_bounds__(256) void select_gather_kernel(VocabRows v, GatherArgs<T> g, uint8_t* __restrict__ flags, int* __restrict__ list,
+                                                            int* __restrict__ place, RowResults zero, PlanLimits lim, VocabPlan* __restrict__ plan) {
+    __shared__ unsigned long long masks[SELECT_ROWS / 64];
+    __shared__ int found[2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x;
+    const bool first = blockIdx.x == 0;
+    int f[SELECT_ROWS / 256];
+#pragma unroll
+    for (int q = 0; q < SELECT_ROWS / 256; ++q) {
+        const int r = q * 256 + tid;
+        f[q] = 0;
+        if (r < v.M) {
+            if (v.labels && in_vocab(v.labels[r], v.V)) f[q] = HAS_LABEL;
+            for (int k = 0; k < v.K; ++k)
+                if (teacher_counts(v.idx[(int64_t)r * v.K + k], v.logits[(int64_t)r * v.K + k], v.V)) f[q] |= HAS_TEACHER;
+        }
+        const unsigned long long m = __ballot(f[q] != 0);
+        if (lane == 0) masks[q * 4 + wave] = m;
+    }
+    __syncthreads();
+    int count = 0;
+#pragma unroll
+    for (int q = 0; q < SELECT_ROWS / 64; ++q) {
+        const unsigned long long m = masks[q];
+        const int before = count, mine = __popcll(m & ((1ull << lane) - 1));
+        count += __popcll(m);
+        const bool on = m >> lane & 1;
+        if ((q & 3) == wave) {
+            const int r = q * 64 + lane, rank = before + mine;
+            if (on && rank == i) { found[0] = r; found[1] = f[q >> 2]; }
+            if (first && r < v.M) {
+                flags[r] = (uint8_t)f[q >> 2];
+                place[r] = on ? rank : -1;
+                if (on) {
+                    list[rank] = r;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (zero.p[k]) zero.p[k][r] = 0.f;
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (first && wave == 0) write_plan(count, v.V, lim, plan, lane);
+    const bool live = i < count;
+    gather_row<T, P>(v, g, i, live, live ? found[0] : 0, live ? found[1] : 0);
 }
 
 // The teacher's probabilities of a row, entry e = 1 + lane + 64 q in p[q] (0: none), and log p_k = t_k / tau - log_norm.
@@ -228,9 +293,74 @@ __device__ __forceinline__ Teacher teacher_of(const VocabRows& v, int r, int lan
 // ---------------------------------------------------------------------------------
 // losses
 // ---------------------------------------------------------------------------------
-// The statistics of 64 rows that count joined, and their losses.  stats: [strips][N][Mp] = maximum m of a strip, sums of
-// exp(z - m) and exp((z - m) / tau), the second with N = 3 only, the first in its place if only the teacher's loss is wanted.  A lane
-// per row and 16 wavefronts over the strips; then a wavefront per row over the teacher's entries.
+// The divergence of a row from its teacher and its lse_tau, by a wavefront; top + log_s / inv_tau is the latter times tau.
+__device__ __forceinline__ void teacher_loss(const VocabRows& v, int r, const float* z, float top, float log_s, int lane, float* kd, float* lse_tau) {
+    const Teacher t = teacher_of(v, r, lane);
+    float sum = 0.f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        if (t.p[q] != 0.f) sum += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - top) * v.inv_tau - log_s));
+    *kd = wave_sum(sum) / (v.inv_tau * v.inv_tau);
+    *lse_tau = top * v.inv_tau + log_s;
+}
+
+// The statistics of a row joined, and its losses, a workgroup per row: for few rows.  stats: see FewRows and losses_kernel.
+template <int N>
+__global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t stat_row, int64_t stat_kind,
+                                                         const float* __restrict__ zs, const uint8_t* __restrict__ flags, RowResults out) {
+    __shared__ float sh[3][4];
+    const int i = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    if (i >= v.plan->count) return;
+    float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
+    const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
+    const float* at = stats + i * stat_row;
+    float m = -INFINITY, s0 = 0.f, s1 = 0.f;
+    for (int p0 = threadIdx.x; p0 < strips; p0 += 1024) {
+        float a[4][N];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int k = 0; k < N; ++k) a[u][k] = p0 + 256 * u < strips ? at[k * stat_kind + p0 + 256 * u] : k ? 0.f : -INFINITY;
+        const float top = fmaxf(fmaxf(fmaxf(a[0][0], a[1][0]), fmaxf(a[2][0], a[3][0])), m);
+        if (top == -INFINITY) continue;
+        s0 *= expf((m - top) * rate0);
+        if (N == 3) s1 *= expf((m - top) * v.inv_tau);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            s0 += a[u][1] * expf((a[u][0] - top) * rate0);
+            if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - top) * v.inv_tau);
+        }
+        m = top;
+    }
+    const float wm = wave_max(m), d = wm == -INFINITY ? 0.f : m - wm;
+    s0 = wave_sum(s0 * expf(d * rate0));
+    if (N == 3) s1 = wave_sum(s1 * expf(d * v.inv_tau));
+    if (lane == 0) { sh[0][w] = wm; sh[1][w] = s0; sh[2][w] = s1; }
+    __syncthreads();
+    if (w) return;
+    const float top = fmaxf(fmaxf(sh[0][0], sh[0][1]), fmaxf(sh[0][2], sh[0][3]));
+    float t0 = 0.f, t1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        t0 += sh[1][k] * expf((sh[0][k] - top) * rate0);
+        if (N == 3) t1 += sh[2][k] * expf((sh[0][k] - top) * v.inv_tau);
+    }
+    const float log0 = logf(t0), log1 = N == 3 ? logf(t1) : log0;
+    const int r = v.list[i];
+    const float* z = zs + (int64_t)i * (v.K + 1);
+    const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
+    float kd = 0.f, l1 = 0.f;
+    if (loss_kd && (flags[r] & HAS_TEACHER)) teacher_loss(v, r, z, top, log1, lane, &kd, &l1);
+    if (lane == 0) {
+        if (loss_ce) loss_ce[r] = has ? log0 + (top - z[0]) : 0.f;
+        lse[r] = has ? top + log0 : 0.f;
+        if (loss_kd) { loss_kd[r] = kd; lse_tau[r] = l1; }
+    }
+}
+
+// The same for 64 rows per workgroup.  stats: [strips][N][Mp] = maximum m of a strip, sums of exp(z - m) and exp((z - m) / tau), the
+// second with N = 3 only, the first in its place if only the teacher's loss is wanted.  A lane per row and 16 wavefronts over
+// the strips; then a wavefront per row over the teacher's entries.
 template <int N>
 __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t Mp, const float* __restrict__ zs,
                                                       const uint8_t* __restrict__ flags, RowResults out) {
@@ -282,17 +412,8 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
     if (!loss_kd) return;
     for (int k = w; k < 64 && i0 + k < count; k += 16) {
         const int i = i0 + k, r = v.list[i];
-        const float top = row[0][k], log_s = row[2][k];
         float kd = 0.f, l = 0.f;
-        if (flags[r] & HAS_TEACHER) {
-            const float* z = zs + (int64_t)i * (v.K + 1);
-            const Teacher t = teacher_of(v, r, lane);
-            l = top * v.inv_tau + log_s;
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                if (t.p[q] != 0.f) kd += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - top) * v.inv_tau - log_s));
-            kd = wave_sum(kd) / (v.inv_tau * v.inv_tau);
-        }
+        if (flags[r] & HAS_TEACHER) teacher_loss(v, r, zs + (int64_t)i * (v.K + 1), row[0][k], row[2][k], lane, &kd, &l);
         if (lane == 0) { loss_kd[r] = kd; lse_tau[r] = l; }
     }
 }
@@ -361,52 +482,10 @@ __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float
 }
 
 // ---------------------------------------------------------------------------------
-// float32: a piece of the vocabulary with its logits in memory
+// few rows in float32
 // ---------------------------------------------------------------------------------
-// One workgroup per row: maximum and sums of a piece (n entries, pitch ld).
-__global__ __launch_bounds__(256) void piece_stats_kernel(const float* __restrict__ z, int64_t ld, int n, const float* __restrict__ bias,
-                                                          const VocabPlan* __restrict__ plan, float inv_tau, int64_t Mp, float* __restrict__ stats) {
-    __shared__ float sh[3][4];
-    const int i = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (i >= plan->count) return;
-    const float* row = z + (int64_t)i * ld;
-    float m = -INFINITY;
-    for (int c = threadIdx.x; c < n; c += 256) m = fmaxf(m, row[c] + (bias ? bias[c] : 0.f));
-    m = wave_max(m);
-    if (lane == 0) sh[0][w] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(sh[0][0], sh[0][1]), fmaxf(sh[0][2], sh[0][3]));
-    const float ref = m == -INFINITY ? 0.f : m;
-    float s0 = 0.f, s1 = 0.f;
-    for (int c = threadIdx.x; c < n; c += 256) {
-        const float d = row[c] + (bias ? bias[c] : 0.f) - ref;
-        s0 += expf(d);
-        s1 += expf(d * inv_tau);
-    }
-    s0 = wave_sum(s0);
-    s1 = wave_sum(s1);
-    if (lane == 0) { sh[1][w] = s0; sh[2][w] = s1; }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        stats[i] = m;
-        stats[Mp + i] = (sh[1][0] + sh[1][1]) + (sh[1][2] + sh[1][3]);
-        stats[2 * Mp + i] = (sh[2][0] + sh[2][1]) + (sh[2][2] + sh[2][3]);
-    }
-}
-
-// The dense part of dz in the place of the logits, zeros in the columns behind the piece and the rows behind the last one that counts.
-__global__ __launch_bounds__(256) void piece_dz_kernel(float* z, int64_t ld, int n, const float* __restrict__ bias, const VocabPlan* __restrict__ plan,
-                                                       const float4* __restrict__ coef, float inv_tau) {
-    const int across = (int)((ld + 255) / 256), i = blockIdx.x / across, c = (blockIdx.x - i * across) * 256 + threadIdx.x;
-    if (c >= ld) return;
-    float d = 0.f;
-    if (i < plan->count && c < n) d = dense_dz(coef[i], z[(int64_t)i * ld + c] + (bias ? bias[c] : 0.f), inv_tau);
-    z[(int64_t)i * ld + c] = d;
-}
-
-// Column sums of a piece of dz: 64 columns per workgroup, 16 wavefronts over the rows.
-__global__ __launch_bounds__(1024) void piece_colsum_kernel(const float* __restrict__ dz, int64_t ld, int n, const VocabPlan* __restrict__ plan,
-                                                            float* __restrict__ out) {
+// Column sums of dz: 64 columns per workgroup, 16 wavefronts over the rows.
+__global__ __launch_bounds__(1024) void db_kernel(const float* __restrict__ dz, int64_t ld, int n, const VocabPlan* __restrict__ plan, float* __restrict__ out) {
     __shared__ float sh[16][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, count = plan->count;
     float s = 0.f;
@@ -419,14 +498,14 @@ __global__ __launch_bounds__(1024) void piece_colsum_kernel(const float* __restr
         out[c] = s;
     }
 }
-
-__global__ __launch_bounds__(256) void add_kernel(const float* __restrict__ more, int64_t n, float* __restrict__ acc) {
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c < n) acc[c] += more[c];
-}
-__global__ __launch_bounds__(256) void copy_kernel(const float* __restrict__ src, int valid, int total, float* __restrict__ dst) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c < total) dst[c] = c < valid ? src[c] : 0.f;
+// The last n < 4 rows of dW, which the product in fours leaves: out[v][d] = sum over i of dz[i][v] x[i][d].
+__global__ __launch_bounds__(256) void dw_rest_kernel(const float* __restrict__ dz, int64_t ld, const float* __restrict__ x, int D, int n,
+                                                      const VocabPlan* __restrict__ plan, float* __restrict__ out) {
+    const int c = blockIdx.x * 256 + threadIdx.x, e = c / D, d = c - e * D, count = plan->count;
+    if (e >= n) return;
+    float s = 0.f;
+    for (int i = 0; i < count; ++i) s = fmaf(dz[(int64_t)i * ld + e], x[(int64_t)i * D + d], s);
+    out[c] = s;
 }
 
 // dX[r] from the sums of its place, zeros for a row that does not count.
@@ -462,62 +541,54 @@ static int vocab_check(const rev_vocab_cfg* c) {
     return REV_OK;
 }
 
-// float32: by parts from PARTS_ROWS rows on
-constexpr int PARTS_ROWS = 128;
-static bool takes_parts(const rev_vocab_cfg& c) { return c.rows > PARTS_ROWS; }
+// Up to FEW_ROWS rows the logits come from vocab_few.hip, and float32 takes the float32 products of the stack.
+constexpr int FEW_ROWS = 128;
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // dz of a piece: 256 MB, what the memory-side cache holds, or 256 entries of all rows if that is more
 constexpr int64_t VOCAB_DZ_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, more, total;
-    int64_t Mp;
+    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, total;
+    int64_t Mp, ldz;                 // ldz: float32 products
+    bool few;
     int parts;                       // bf16 parts of an operand of the products; 0: float32 products (gemm_f32.hip)
-    int Dp, strips, pieces;          // parts: most pieces that a plan may have
-    int Vc, rest;                    // float32: width of a piece, entries left over behind whole multiples of 4 (the last piece)
+    int Dp, strips, pieces;          // pieces: most that a plan may have
     PlanLimits lim;
 };
 static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     VocabLayout L = {};
-    L.parts = c.mode == REV_MODE_BF16 ? 1 : takes_parts(c) ? 3 : 0;
     const int64_t M = c.rows, D = c.d_model, V = c.vocab;
+    L.few = M <= FEW_ROWS;
+    L.parts = c.mode == REV_MODE_BF16 ? 1 : L.few ? 0 : 3;
+    L.Dp = L.parts ? (int)up(D, 128) : c.d_model;
+    L.Mp = L.parts ? up(M, 256) : M;
+    L.strips = (int)(L.few ? (V + 63) / 64 : (V + 255) / 256 * 2);
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
     L.plan = take(sizeof(VocabPlan));
     L.flags = take(M);
     L.place = take(4 * M);
     L.list = take(4 * M);
+    L.coef = take(16 * M);
     L.label_dz = take(8 * M);
     L.zs = take(4 * M * (c.top_k + 1));
+    L.stats = take(12 * (L.few ? M : L.Mp) * L.strips);
     if (L.parts) {
-        L.Mp = up(M, 256);
-        L.Dp = (int)up(D, 128);
-        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), L.Mp * up(V, 256));
+        const int64_t all = L.Mp * up(V, 256);
+        L.lim.dz = L.few ? all : std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
         L.lim.tiles_d = (int)((D + 255) / 256);
         L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
         L.pieces = (int)((V + least - 1) / least);
-        L.strips = (int)((V + 255) / 256) * 2;
-        L.coef = take(16 * M);
-        L.stats = take(12 * L.Mp * L.strips);
         L.xc = take(2 * L.parts * L.Mp * L.Dp);
-        L.w = L.Dp != D || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
+        L.w = (!L.few && L.Dp != D) || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
         L.dz = take(2 * L.parts * L.lim.dz);
         L.acc = take((int64_t)L.lim.slots * 65536 * 4);
     } else {
-        L.Mp = up(M, 64);
-        L.Dp = c.d_model;
-        const int64_t whole = V / 4 * 4;
-        L.Vc = (int)std::min(std::max(VOCAB_DZ_BYTES / 4 / L.Mp / 256 * 256, (int64_t)256), std::max<int64_t>(whole, 4));
-        L.rest = (int)(V - whole);
-        L.pieces = L.strips = (int)((whole + L.Vc - 1) / L.Vc) + (L.rest ? 1 : 0);
-        L.coef = take(16 * M);
-        L.stats = take(12 * L.Mp * L.strips);
-        L.xc = take(4 * L.Mp * D);
-        L.w = take(4 * 4 * D);
-        L.dz = take(4 * L.Mp * L.Vc);
-        L.acc = take(4 * L.Mp * D);
-        L.more = take(4 * std::max<int64_t>(4, L.pieces > 1 ? L.Mp : 0) * D);
+        L.ldz = up(V, 4);
+        L.xc = take(4 * M * D);
+        L.dz = take(4 * M * L.ldz);
+        L.acc = take(4 * M * D);
     }
     L.total = at;
     return L;
@@ -551,24 +622,40 @@ struct VocabRunner {
     bool dual() const { return losses() == (LOSS_CE | LOSS_KD) && c.temperature != 1.f; }
 
     // the rows that count, their logits at named entries, and in the backward pass (cot.lse) what their dense parts are made of
-    int prepare(const void* X, const RowResults& zero, const Cotangents& cot) {
+    template <int P> int prepare(const void* X, const RowResults& zero, const Cotangents& cot) {
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
+        const GatherArgs<T> g = {params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), cot, cot.lse ? at<float4>(L.coef) : nullptr,
+                                 cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr};
+        const dim3 rows((unsigned)L.Mp), block(256);
+        if (M <= SELECT_ROWS && (int64_t)M * (v.K + 1) <= SELECT_ENTRIES) {
+            LAUNCH((select_gather_kernel<T, P>), rows, block, v, g, at<uint8_t>(L.flags), at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
+            return REV_OK;
+        }
         if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
         LAUNCH(select_rows_kernel, dim3(1), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
-        float4* coef = cot.lse ? at<float4>(L.coef) : nullptr;
-        LabelDz* label_dz = cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr;
-        const dim3 grid((unsigned)L.Mp), block(256);
-        if (L.parts)
-            LAUNCH((gather_kernel<T, kParts>), grid, block, v, params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), flags(), cot, coef, label_dz);
-        else
-            LAUNCH((gather_kernel<T, 0>), grid, block, v, params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), flags(), cot, coef, label_dz);
+        LAUNCH((gather_kernel<T, P>), rows, block, v, g, flags());
         return REV_OK;
     }
-    int join(const RowResults& out, bool three) {
-        ProfScope ps(K_REDUCE, s, 12.0 * L.Mp * L.strips);
-        if (three) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
+    int prepare(const void* X, const RowResults& zero, const Cotangents& cot) { return L.parts ? prepare<kParts>(X, zero, cot) : prepare<0>(X, zero, cot); }
+
+    int join(const RowResults& out) {
+        ProfScope ps(K_REDUCE, s, 12.0 * M * L.strips);
+        const int64_t kind = L.strips;
+        if (L.few && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        else if (L.few) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
         else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
         return REV_OK;
+    }
+    FewRows<T> few_args() {
+        FewRows<T> f = {};
+        f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
+        f.label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); f.dz = at<T>(L.dz);
+        f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
+        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.inv_tau = v.inv_tau;
+        f.rows_x = (int)L.Mp;
+        f.rows_out = L.parts ? (int)up(M, 128) : M;                // dw goes over whole 128 rows
+        return f;
     }
 
     // ---- products of bf16 parts ----
@@ -591,7 +678,7 @@ struct VocabRunner {
         VocabGemm g;
         RC(gemm_args(&g));
         RC(vocab_logits<T>(s, g, false, dual(), L.Mp / 256 * ((V + 255) / 256)));
-        return join(out, dual());
+        return join(out);
     }
     int backward_parts(T* dX, void* dparams) {
         VocabGemm g;
@@ -600,7 +687,8 @@ struct VocabRunner {
             // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
             const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
             g.piece = k;
-            RC(vocab_logits<T>(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
+            if (L.few) RC(few_logits<T>(s, few_args(), true, false, M, up(V, 256)));
+            else RC(vocab_logits<T>(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
             if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
                               (int64_t)0, L.lim.dz);
             if (dX) RC(vocab_dx<T>(s, g, L.lim.slots));
@@ -610,59 +698,31 @@ struct VocabRunner {
     }
 
     // ---- float32 products ----
-    struct Piece { int v0, n, width; const float* w; };              // first entry, entries, width (a multiple of 4), its rows of W
-    int piece(int k, Piece* p) {
-        const bool last = L.rest && k == L.pieces - 1;
-        p->v0 = last ? V - L.rest : k * L.Vc;
-        p->n = last ? L.rest : std::min(L.Vc, V / 4 * 4 - p->v0);
-        p->width = last ? 4 : p->n;
-        p->w = (const float*)params + (int64_t)p->v0 * D;
-        if (last) {
-            LAUNCH(copy_kernel, blocks_of(4 * D, 256), dim3(256), p->w, L.rest * D, 4 * D, at<float>(L.w));
-            p->w = at<float>(L.w);
-        }
-        Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = at<float>(L.dz); e.ldo = p->width; e.solo = true;
-        return gemm_nt_f32(s, at<float>(L.xc), D, p->w, D, (int)L.Mp, p->width, D, e);
-    }
-    int forward_f32(const RowResults& out) {
-        for (int k = 0; k < L.pieces; ++k) {
-            Piece p;
-            RC(piece(k, &p));
-            LAUNCH(piece_stats_kernel, dim3(M), dim3(256), at<float>(L.dz), (int64_t)p.width, p.n, bias() ? (const float*)bias() + p.v0 : nullptr, v.plan, v.inv_tau,
-                   L.Mp, at<float>(L.stats) + (int64_t)k * 3 * L.Mp);
-        }
-        return join(out, true);
-    }
     int backward_f32(float* dX, float* dparams) {
-        float *dz = at<float>(L.dz), *acc = at<float>(L.acc), *more = at<float>(L.more);
-        for (int k = 0; k < L.pieces; ++k) {
-            Piece p;
-            RC(piece(k, &p));
-            LAUNCH(piece_dz_kernel, dim3((unsigned)((p.width + 255) / 256 * L.Mp)), dim3(256), dz, (int64_t)p.width, p.n, bias() ? (const float*)bias() + p.v0 : nullptr,
-                   v.plan, at<float4>(L.coef), v.inv_tau);
-            LAUNCH((sparse_dz_kernel<float, 1>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), p.v0, p.n, dz, (int64_t)p.width, (int64_t)0);
-            if (dX) {
-                Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = k ? more : acc; e.ldo = D; e.solo = true;
-                RC(gemm_nn_f32(s, dz, p.width, p.w, D, (int)L.Mp, D, p.width, e));
-                if (k) LAUNCH(add_kernel, blocks_of(L.Mp * D, 256), dim3(256), more, L.Mp * D, acc);
-            }
-            if (dparams) {
-                float* dw = dparams + (int64_t)p.v0 * D;
-                const WgradF32Item it = {dz, p.width, at<float>(L.xc), D, p.width, D, p.width == p.n ? dw : more, nullptr};
-                RC(gemm_wgrad_f32_group(s, &it, 1, (int)L.Mp));
-                if (p.width != p.n) LAUNCH(copy_kernel, blocks_of(p.n * D, 256), dim3(256), more, p.n * D, p.n * D, dw);
-                if (c.bias) LAUNCH(piece_colsum_kernel, blocks_of(p.n, 64), dim3(1024), dz, (int64_t)p.width, p.n, v.plan, dparams + (int64_t)V * D + p.v0);
-            }
+        float *dz = at<float>(L.dz), *acc = at<float>(L.acc), *x = at<float>(L.xc);
+        const float* w = (const float*)params;
+        RC(few_logits<T>(s, few_args(), true, false, M, L.ldz));
+        if (v.idx) LAUNCH((sparse_dz_kernel<float, 0>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), 0, V, dz, L.ldz, (int64_t)0);
+        if (dX) {
+            Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = acc; e.ldo = D; e.solo = true;
+            RC(gemm_nn_f32(s, dz, L.ldz, w, D, M, D, V, e));
+            LAUNCH(dx_rows_kernel, blocks_of((int64_t)M * D / 4, 256), dim3(256), acc, v.place, M, D, dX);
         }
-        if (dX) LAUNCH(dx_rows_kernel, blocks_of((int64_t)M * D / 4, 256), dim3(256), acc, v.place, M, D, dX);
+        if (dparams) {
+            const int whole = V / 4 * 4;
+            const WgradF32Item it = {dz, L.ldz, x, D, whole, D, dparams, nullptr};
+            if (whole) RC(gemm_wgrad_f32_group(s, &it, 1, M));
+            if (V > whole) LAUNCH(dw_rest_kernel, blocks_of((V - whole) * D, 256), dim3(256), dz + whole, L.ldz, x, D, V - whole, v.plan, dparams + (int64_t)whole * D);
+            if (c.bias) LAUNCH(db_kernel, blocks_of(V, 64), dim3(1024), dz, L.ldz, V, v.plan, dparams + (int64_t)V * D);
+        }
         return REV_OK;
     }
 
     int forward(const void* X, const RowResults& out) {
         RC(prepare(X, out, Cotangents{}));
-        if (L.parts) return forward_parts(out);
-        if constexpr (kParts == 3) return forward_f32(out);
-        return REV_OK;
+        if (!L.few) return forward_parts(out);
+        RC(few_logits<T>(s, few_args(), false, dual(), M, V));
+        return join(out);
     }
     int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
         RC(prepare(X, RowResults{}, cot));
