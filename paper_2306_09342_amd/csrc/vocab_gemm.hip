@@ -18,11 +18,12 @@
 // that finds no tile ends at once.
 #include "mfma.h"
 #include "vocab.h"
+#include <algorithm>
 #include <type_traits>
 
 namespace rev {
 
-constexpr int VG_PART = 16384, VG_LDS = 8 * VG_PART;
+constexpr int VG_PART = 16384, VG_LDS = 8 * VG_PART, VG_SIDE = 2048;
 template <int V> using vg_int = std::integral_constant<int, V>;
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
@@ -38,17 +39,6 @@ template <int P> struct Parts {
     __device__ __forceinline__ int within(int kt, int t) const { return P == 1 ? kt : kt - t * stages; }
     __device__ __forceinline__ int total() const { return P == 1 ? stages : 6 * stages; }
 };
-// A value of dz, or three parts of it, `part` apart.
-template <int P> __device__ __forceinline__ void store_dz(bf16* at, int64_t part, float v) {
-    if constexpr (P == 1) {
-        *at = from_f<bf16>(v);
-    } else {
-        bf16 q[3];
-        split3(v, q);
-        at[0] = q[0]; at[part] = q[1]; at[2 * part] = q[2];
-    }
-}
-
 struct TileLane {
     int lane, wave, wm, wn, g, fr;
     __device__ __forceinline__ TileLane() {
@@ -67,17 +57,26 @@ struct TileLane {
 // acc[h][j][i] += the products of B half h (32-entry block i of this wavefront's 64) and A half j over nst stages, an even number,
 // at least two.  Accumulator register v of lane (g, fr) is B entry h 128 + wm 64 + i 32 + 8 (v / 4) + 4 g + v % 4, A entry
 // j 128 + wn 32 + fr.  AKM / BKM: the operand lies across the contraction.  issue_x(half, stage, address in LDS) requests a part.
+// request_stages has asked for the first two stages; what the wavefront has asked of memory since then is only waited for longer.
+// In LDS: B0 B1 of stage 0, B0 B1 of stage 1, then the same of A.
+template <class IssueA, class IssueB>
+__device__ __forceinline__ void request_stages(unsigned char* smem, const TileLane& t, const IssueA& issue_a, const IssueB& issue_b) {
+    const unsigned lds_w = (unsigned)(uintptr_t)LDS_PTR(unsigned char, smem) + t.wave * 1024;
+    using H0 = vg_int<0>; using H1 = vg_int<1>;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+        const unsigned b = lds_w + kt * (2 * VG_PART), a = b + 4 * VG_PART;
+        issue_b(H0{}, kt, b); issue_a(H0{}, kt, a); issue_a(H1{}, kt, a + VG_PART); issue_b(H1{}, kt, b + VG_PART);
+    }
+}
 template <bool AKM, bool BKM, class IssueA, class IssueB>
 __device__ __forceinline__ void tile_products(unsigned char* smem, const TileLane& t, const IssueA& issue_a, const IssueB& issue_b, int nst,
                                               f32x16_t (&acc)[2][2][2]) {
     const unsigned lds0 = (unsigned)(uintptr_t)LDS_PTR(unsigned char, smem), lds_w = lds0 + t.wave * 1024;
     const int grp = t.wave >> 2;
-    // in LDS B0 B1 of stage 0, B0 B1 of stage 1, then the same of A
     auto request_b = [&](auto half, int kt) { issue_b(half, kt, lds_w + (kt & 1) * (2 * VG_PART) + decltype(half)::value * VG_PART); };
     auto request_a = [&](auto half, int kt) { issue_a(half, kt, lds_w + 4 * VG_PART + (kt & 1) * (2 * VG_PART) + decltype(half)::value * VG_PART); };
     using H0 = vg_int<0>; using H1 = vg_int<1>;
-    request_b(H0{}, 0); request_a(H0{}, 0); request_a(H1{}, 0); request_b(H1{}, 0);
-    request_b(H0{}, 1); request_a(H0{}, 1); request_a(H1{}, 1); request_b(H1{}, 1);
 
     unsigned a_addr[4], b_addr[4];
 #pragma unroll
@@ -201,6 +200,21 @@ __device__ __forceinline__ void tile_products(unsigned char* smem, const TileLan
     if (!grp) barrier();
 }
 
+// The tiles of a launch of as many workgroups as run at once: each XCD (workgroups b, b + 8, ...) has one run of them, in which its
+// workgroups go side by side, so that tiles which share an operand meet in its L2.
+struct TileRun {
+    int start, size, next, step;
+    __device__ __forceinline__ TileRun(int tiles) {
+        const int x = blockIdx.x & 7, per = tiles >> 3, rem = tiles & 7;
+        start = x * per + min(x, rem);
+        size = per + (x < rem);
+        next = blockIdx.x >> 3;
+        step = ((int)gridDim.x - x + 7) >> 3;
+    }
+    __device__ __forceinline__ bool done() const { return next >= size; }
+    __device__ __forceinline__ int tile() const { return start + next; }
+};
+
 __device__ __forceinline__ void clear(f32x16_t (&acc)[2][2][2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -235,10 +249,12 @@ __device__ __forceinline__ void store_eights(bf16* out, const f32x16_t& d, bool 
     }
 }
 
-// The logits of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so that neither
-// costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the sums are of
-// exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are kept side by side.
-// What bounds it: see the file's head; the epilogue is 128 exponentials a lane (twice that with DUAL), which nothing overlaps.
+// The logits of tiles of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so
+// that neither costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the
+// sums are of exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are
+// kept side by side.  Backward: dz, with the label's entry in its place where labels alone are named.
+// What bounds it: see the file's head; the epilogue is 128 exponentials a lane (twice that with DUAL).  The first two stages
+// of the next tile are under way meanwhile, and its bias.
 template <bool GRAD, bool DUAL, int P>
 __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
@@ -246,25 +262,54 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     const VocabPlan pl = *p.plan;
     const int tiles_m = __builtin_amdgcn_readfirstlane(pl.rows >> 8);
     const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.V, v0 = GRAD ? width * p.piece : 0, n = min(width, p.V - v0);
-    const int tiles_n = n > 0 ? (n + 255) >> 8 : 0, tiles = tiles_m * tiles_n;
-    if ((int)blockIdx.x >= tiles) return;
-    const int tile = xcd_remap(blockIdx.x, tiles);
-    const int gn = tiles_n <= 6 ? tiles_n : 4, per_group = gn * tiles_m, tg = tile / per_group, in_grp = tile - tg * per_group;
-    const int gw = min(gn, tiles_n - tg * gn);
-    const int m0 = __builtin_amdgcn_readfirstlane((in_grp / gw) * 256), n0 = __builtin_amdgcn_readfirstlane((tg * gn + in_grp % gw) * 256);
-
+    const int tiles_n = n > 0 ? (n + 255) >> 8 : 0;
+    TileRun run(tiles_m * tiles_n);
+    if (run.done()) return;
+    const int gn = tiles_n <= 6 ? tiles_n : 4, per_group = gn * tiles_m;
     const int64_t lda = p.Dp, ldb = p.Dp;
     const unsigned va = (unsigned)(t.row_along() * lda * 2 + t.byte_along());
-    const int last = n - 1 - n0;                                   // rows of W beyond it read that one again
-    const char* a_base = reinterpret_cast<const char*>(p.x + m0 * lda);
-    const char* b_base = reinterpret_cast<const char*>(p.wp + (int64_t)(v0 + n0) * ldb);
-    unsigned vb[2][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) vb[h][q] = (unsigned)(min(h * 128 + q * 64 + t.row_along(), last) * ldb * 2 + t.byte_along());
     const Parts<P> parts{p.Dp >> 6};
     const int64_t part_a = p.Mp * lda * 2, part_b = p.V * ldb * 2;
+
+    // the tile whose operands are being requested, and what its epilogue will need
+    int m0, n0;
+    const char *a_base, *b_base;
+    unsigned vb[2][2];
+    // The rest goes to 2 KB of LDS of the wavefront's own: the bias of its 2 x 64 entries, {coefficients, label, dz there} of its 2 x 32
+    // rows.  (Registers for it would be short of 20 in the main loop.)
+    typedef typename std::conditional<P == 1, u32x2_t, f32x4_t>::type quad_t;
+    unsigned char* side = smem + VG_LDS + t.wave * VG_SIDE;
+    const unsigned side_lds = (unsigned)(uintptr_t)LDS_PTR(unsigned char, side);
+    const int quad_end = p.V - v0 - 4;
+    const bool biased = p.bias != nullptr, biased_quads = biased && p.V >= 4;
+    auto take_tile = [&]() {
+        const int tile = run.tile(), tg = tile / per_group, in_grp = tile - tg * per_group, gw = min(gn, tiles_n - tg * gn);
+        m0 = __builtin_amdgcn_readfirstlane((in_grp / gw) * 256);
+        n0 = __builtin_amdgcn_readfirstlane((tg * gn + in_grp % gw) * 256);
+        a_base = reinterpret_cast<const char*>(p.x + m0 * lda);
+        b_base = reinterpret_cast<const char*>(p.wp + (int64_t)(v0 + n0) * ldb);
+        const int last = n - 1 - n0;                               // rows of W beyond it read that one again
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) vb[h][q] = (unsigned)(min(h * 128 + q * 64 + t.row_along(), last) * ldb * 2 + t.byte_along());
+        if (biased_quads) {                                        // words beyond the vocabulary's whole quads are not used: its first
+            const int c = v0 + n0 + (t.lane >> 5) * 128 + t.wm * 64 + (P == 1 ? 2 : 1) * t.fr;
+#pragma unroll
+            for (int q = 0; q < (P == 1 ? 1 : 2); ++q) {
+                const int at = c + 32 * q;
+                dma4_sbase(p.bias, (at <= p.V - (P == 1 ? 2 : 1) ? at : 0) * (P == 1 ? 2 : 4), side_lds + 256 * q);
+            }
+        }
+        if (GRAD) {
+            const int row = m0 + (t.lane >> 5) * 128 + t.wn * 32 + t.fr;
+            dma16_sbase(p.coef, row * 16, side_lds + 512);
+            if (p.label_dz) {
+                dma4_sbase(p.label_dz, row * 8, side_lds + 1536);
+                dma4_sbase(p.label_dz, row * 8 + 4, side_lds + 1792);
+            }
+        }
+    };
     auto issue_a = [&](auto half, int kt, unsigned lds) {
         const int term = parts.term(kt);
         const char* src = a_base + parts.a(term) * part_a + decltype(half)::value * 256 * lda + parts.within(kt, term) * 128;
@@ -278,128 +323,146 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
         dma16_sbase(src, vb[h][0], lds);
         dma16_sbase(src, vb[h][1], lds + 8192);
     };
-    f32x16_t acc[2][2][2];
-    {
-        // four entries at a time; the last few of the vocabulary by themselves
-        const int quad_end = p.V - v0 - 4;
-        auto bias_at = [&](int c) {
-            return P == 1 ? to_f(reinterpret_cast<const bf16*>(p.bias)[v0 + c]) : reinterpret_cast<const float*>(p.bias)[v0 + c];
-        };
+    take_tile();
+    request_stages(smem, t, issue_a, issue_b);
+    for (;;) {
+        f32x16_t acc[2][2][2];
+        wait_vm<16>();                                             // what was asked for ahead of the two stages
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * k + 4 * t.g;
-                    f32x4_t b = {0.f, 0.f, 0.f, 0.f};
-                    if (p.bias && c <= quad_end) {
-                        if (P == 1) {
-                            const u32x2_t u = *reinterpret_cast<const u32x2_t*>(reinterpret_cast<const bf16*>(p.bias) + v0 + c);
-                            b = f32x4_t{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16),
-                                        __uint_as_float(u[1] & 0xFFFF0000u)};
-                        } else {
-                            b = *reinterpret_cast<const f32x4_t*>(reinterpret_cast<const float*>(p.bias) + v0 + c);
-                        }
-                    }
+                    // in memory's order for bf16 (two entries per word, 32 words of each half), by 32 entries for float32
+                    const int c = i * 32 + 8 * k + 4 * t.g;
+                    quad_t b = quad_t{};
+                    if (biased_quads) b = *reinterpret_cast<const quad_t*>(side + (P == 1 ? h * 128 + c * 2 : i * 256 + h * 128 + (c & 31) * 4));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[h][0][i][4 * k + e] = b[e];
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (P == 1) acc[h][0][i][4 * k + e] = __uint_as_float(e & 1 ? b[e >> 1] & 0xFFFF0000u : b[e >> 1] << 16);
+                        else acc[h][0][i][4 * k + e] = b[e];
+                    }
                 }
         if (n0 + 256 > n) {                                        // the vocabulary's or the piece's last tile
+            const int first = n0 + t.wm * 64 + 4 * t.g, beyond = n - first, part_quad = ((quad_end + 4) & ~3) - first;
+            const char* from = reinterpret_cast<const char*>(p.bias) + (int64_t)(v0 + first) * (P == 1 ? 2 : 4);
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int c = n0 + h * 128 + t.wm * 64 + i * 32 + 8 * (v >> 2) + 4 * t.g + (v & 3);
-                        if (c >= n) acc[h][0][i][v] = -INFINITY;
-                        else if (p.bias && (c & ~3) > quad_end) acc[h][0][i][v] = bias_at(c);
+                        const int c = h * 128 + i * 32 + 8 * (v >> 2) + (v & 3);
+                        if (c >= beyond) acc[h][0][i][v] = -INFINITY;
+                        else if (biased && c >= part_quad)         // of a quad that the vocabulary does not fill
+                            acc[h][0][i][v] = P == 1 ? to_f(reinterpret_cast<const bf16*>(from)[c]) : reinterpret_cast<const float*>(from)[c];
                     }
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 2; ++i) acc[h][1][i] = acc[h][0][i];
-    }
-    tile_products<false, false>(smem, t, issue_a, issue_b, parts.total(), acc);
+        const int tm0 = m0, tn0 = n0;
+        tile_products<false, false>(smem, t, issue_a, issue_b, parts.total(), acc);
+        float4 tc[2];
+        LabelDz ty[2];
+        if (GRAD) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                // rows behind the last one that counts: 0 exp(z - infinity)
+                tc[j] = make_float4(0.f, INFINITY, 0.f, INFINITY);
+                ty[j] = {-1, 0.f};
+                if (tm0 + j * 128 + t.wn * 32 + t.fr < pl.count) {
+                    tc[j] = *reinterpret_cast<const float4*>(side + 512 + (j * 32 + t.fr) * 16);
+                    if (p.label_dz) ty[j] = {*reinterpret_cast<const int*>(side + 1536 + (j * 32 + t.fr) * 4),
+                                             *reinterpret_cast<const float*>(side + 1792 + (j * 32 + t.fr) * 4)};
+                }
+            }
+            wait_lds();                                            // the next tile's take their place
+        }
+        run.next += run.step;
+        const bool more = !run.done();
+        if (more) {
+            take_tile();
+            request_stages(smem, t, issue_a, issue_b);
+        }
 
-    if constexpr (!GRAD) {
-        const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
-        const int strip = (n0 >> 7) + t.wm;
+        if constexpr (!GRAD) {
+            const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
+            const int strip = (tn0 >> 7) + t.wm;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            float m = -INFINITY;
+            for (int j = 0; j < 2; ++j) {
+                float m = -INFINITY;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[h][j][i][v]);
-            m = fmaxf(m, __shfl_xor(m, 32, 64));
-            const float ref = m == -INFINITY ? 0.f : m;
-            float s0 = 0.f, s1 = 0.f;
+                        for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[h][j][i][v]);
+                m = fmaxf(m, __shfl_xor(m, 32, 64));
+                const float ref = m == -INFINITY ? 0.f : m;
+                float s0 = 0.f, s1 = 0.f;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                    for (int i = 0; i < 2; ++i)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float d = acc[h][j][i][v] - ref;     // first: a lowest value times a scale may overflow
-                        s0 += __builtin_amdgcn_exp2f(d * e0);
-                        if (DUAL) s1 += __builtin_amdgcn_exp2f(d * e1);
+                        for (int v = 0; v < 16; ++v) {
+                            const float d = acc[h][j][i][v] - ref; // first: a lowest value times a scale may overflow
+                            s0 += __builtin_amdgcn_exp2f(d * e0);
+                            if (DUAL) s1 += __builtin_amdgcn_exp2f(d * e1);
+                        }
+                s0 += __shfl_xor(s0, 32, 64);
+                if (DUAL) s1 += __shfl_xor(s1, 32, 64);
+                if (t.g == 0) {
+                    float* out = p.stats + (int64_t)strip * (DUAL ? 3 : 2) * p.Mp + tm0 + j * 128 + t.wn * 32 + t.fr;
+                    out[0] = m;
+                    out[p.Mp] = s0;
+                    if (DUAL) out[2 * p.Mp] = s1;
+                }
+            }
+        } else {
+            const int64_t ldz = width;
+            const float s0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = tm0 + j * 128 + t.wn * 32 + t.fr;
+                float4 c = tc[j];
+                if (!DUAL && (p.losses & LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
+                bf16* out = p.dz + row * ldz + tn0 + t.wm * 64 + 8 * t.g;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        f32x16_t d;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const float z = acc[h][j][i][v];
+                            d[v] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
+                            if (DUAL) d[v] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[v]);
+                        }
+                        const int at = ty[j].label - (v0 + tn0 + h * 128 + t.wm * 64 + i * 32) - 4 * t.g;
+                        if (__any((unsigned)at < 28u)) {
+#pragma unroll
+                            for (int v = 0; v < 16; ++v)
+                                if (at == 8 * (v >> 2) + (v & 3)) d[v] = ty[j].dz;
+                        }
+#pragma unroll
+                        for (int part = 0; part < P; ++part) {
+                            store_eights(out + part * p.dz_part + h * 128 + i * 32, d);
+                            if (part + 1 < P)
+#pragma unroll
+                                for (int v = 0; v < 16; ++v) {
+                                    const float r = d[v] - to_f(from_f<bf16>(d[v]));
+                                    d[v] = fabsf(r) < INFINITY ? r : 0.f;
+                                }
+                        }
+                        __builtin_amdgcn_sched_barrier(0);         // one block's registers at a time
                     }
-            s0 += __shfl_xor(s0, 32, 64);
-            if (DUAL) s1 += __shfl_xor(s1, 32, 64);
-            if (t.g == 0) {
-                float* out = p.stats + (int64_t)strip * (DUAL ? 3 : 2) * p.Mp + m0 + j * 128 + t.wn * 32 + t.fr;
-                out[0] = m;
-                out[p.Mp] = s0;
-                if (DUAL) out[2 * p.Mp] = s1;
             }
         }
-    } else {
-        const int64_t ldz = width;
-        const float s0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int row = m0 + j * 128 + t.wn * 32 + t.fr;
-            // rows behind the last one that counts: 0 exp(z - infinity)
-            float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
-            if (row < pl.count) c = p.coef[row];
-            if (!DUAL && (p.losses & LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
-            bf16* out = p.dz + row * ldz + n0 + t.wm * 64 + 8 * t.g;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    f32x16_t d;
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const float z = acc[h][j][i][v];
-                        d[v] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
-                        if (DUAL) d[v] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[v]);
-                    }
-#pragma unroll
-                    for (int part = 0; part < P; ++part) {
-                        store_eights(out + part * p.dz_part + h * 128 + i * 32, d);
-                        if (part + 1 < P)
-#pragma unroll
-                            for (int v = 0; v < 16; ++v) {
-                                const float r = d[v] - to_f(from_f<bf16>(d[v]));
-                                d[v] = fabsf(r) < INFINITY ? r : 0.f;
-                            }
-                    }
-                }
-        }
-        if (p.label_dz) {                                          // the labels of this tile, behind its stores
-            const int row = m0 + (int)threadIdx.x;
-            LabelDz y = {-1, 0.f};
-            if (threadIdx.x < 256 && row < pl.count) y = p.label_dz[row];
-            __syncthreads();
-            const int c = y.label - v0;
-            if (y.label >= 0 && c >= n0 && c < n0 + 256 && c < n) store_dz<P>(p.dz + row * ldz + c, p.dz_part, y.dz);
-        }
+        if (!more) break;
     }
 }
 
@@ -452,6 +515,7 @@ __global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
                 dma16_sbase(src, (unsigned)(min(t.row_across() + 32, left) * ldb * 2) + col[h], lds + 8192);
             }
         };
+        request_stages(smem, t, issue_a, issue_b);
         tile_products<false, true>(smem, t, issue_a, issue_b, parts.total(), acc);
     }
 #pragma unroll
@@ -584,6 +648,7 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
             dma16_sbase(src, vb[decltype(half)::value], lds);
             dma16_sbase(src + 64 * ldb, vb[decltype(half)::value], lds + 8192);
         };
+        request_stages(smem, t, issue_a, issue_b);
         tile_products<true, true>(smem, t, issue_a, issue_b, parts.total(), acc);
     }
 #pragma unroll
@@ -617,8 +682,9 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
 
 template <typename... A>
 static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipStream_t s, A... args) {
-    if (int rc = lim.ensure(reinterpret_cast<const void*>(kern), VG_LDS)) return rc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(512), VG_LDS, s, args...);
+    constexpr int lds = VG_LDS + 8 * VG_SIDE;
+    if (int rc = lim.ensure(reinterpret_cast<const void*>(kern), lds)) return rc;
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(512), lds, s, args...);
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
@@ -629,6 +695,7 @@ template <typename T>
 int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks) {
     constexpr int P = parts_of<T>;
     ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+    blocks = std::min<int64_t>(blocks, 256);                       // one per CU
     static LdsLimit lim[4];
     if (grad) return dual ? launch_tiles(vocab_logits_kernel<true, true, P>, lim[0], blocks, s, p) : launch_tiles(vocab_logits_kernel<true, false, P>, lim[1], blocks, s, p);
     return dual ? launch_tiles(vocab_logits_kernel<false, true, P>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false, P>, lim[3], blocks, s, p);

@@ -569,8 +569,8 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.flags = take(M);
     L.place = take(4 * M);
     L.list = take(4 * M);
-    L.coef = take(16 * M);
-    L.label_dz = take(8 * M);
+    L.coef = take(16 * L.Mp);
+    L.label_dz = take(8 * L.Mp);
     L.zs = take(4 * M * (c.top_k + 1));
     L.stats = take(12 * (L.few ? M : L.Mp) * L.strips);
     if (L.parts) {
