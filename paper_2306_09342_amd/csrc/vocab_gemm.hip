@@ -534,33 +534,43 @@ __global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
                 }
 }
 
-// dX[r], 32 columns per thread: the ranges' sums of the row's place added in order; zeros for a row that does not count.
+// dX of the rows that count, 32 columns per thread: the ranges' sums of the row's place added in order.  The workgroups behind `sums`
+// of them clear the rows that do not.  Bound by reading the ranges' sums.
 template <typename T>
-__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const int* __restrict__ place, int M, T* __restrict__ dX) {
-    const int blocks = (p.D + 31) >> 5, r = blockIdx.x * 64 + (threadIdx.x & 63), cb = blockIdx.y * 4 + (threadIdx.x >> 6);
-    if (r >= M || cb >= blocks) return;
-    const int i = place[r], d0 = cb * 32;
-    f32x4_t s[8] = {};
-    if (i >= 0) {
-        const VocabPlan pl = *p.plan;
-        const int tiles_d = (p.D + 255) >> 8, tiles = (pl.rows >> 8) * tiles_d, tile = (i >> 8) * tiles_d + (d0 >> 8);
-        const int h = d0 >> 7 & 1, wm = d0 >> 6 & 1, ib = d0 >> 5 & 1, j = i >> 7 & 1, wn = i >> 5 & 3, fr = i & 31;
-        const float* at = p.acc + (int64_t)tile * 65536 + (wn * 2 + wm) * 8192 + (h * 4 + j * 2 + ib) * 1024 + fr * 4;
-        for (int k = 0; k < pl.splits; k += 4) {
-            f32x4_t v[4][8];
+__global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const int* __restrict__ list, const int* __restrict__ place, int M, int sums,
+                                                            T* __restrict__ dX) {
+    const int blocks = (p.D + 31) >> 5, lane = threadIdx.x & 63, w = threadIdx.x >> 6, groups = (blocks + 3) >> 2;
+    if ((int)blockIdx.x >= sums) {                                 // four rows per wavefront
+        constexpr int E = 16 / sizeof(T);
+        const int r0 = (blockIdx.x - sums) * 16 + w * 4;
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[u][e] = k + u < pl.splits ? *reinterpret_cast<const f32x4_t*>(at + (int64_t)(k + u) * tiles * 65536 + (e >> 1) * 256 + (e & 1) * 128)
-                                                : f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) s[e] += v[u][e];
-        }
+        for (int k = 0; k < 4; ++k)
+            if (r0 + k < M && place[r0 + k] < 0)
+                for (int d = lane * E; d < p.D; d += 64 * E) *reinterpret_cast<u32x4_t*>(dX + (int64_t)(r0 + k) * p.D + d) = u32x4_t{0, 0, 0, 0};
+        return;
     }
-    T* out = dX + (int64_t)r * p.D + d0;
+    const VocabPlan pl = *p.plan;
+    const int rb = blockIdx.x / groups, cb = (blockIdx.x - rb * groups) * 4 + w, i = rb * 64 + lane;
+    if (i >= pl.count || cb >= blocks) return;
+    const int d0 = cb * 32;
+    f32x4_t s[8] = {};
+    const int tiles_d = (p.D + 255) >> 8, tiles = (pl.rows >> 8) * tiles_d, tile = (i >> 8) * tiles_d + (d0 >> 8);
+    const int h = d0 >> 7 & 1, wm = d0 >> 6 & 1, ib = d0 >> 5 & 1, j = i >> 7 & 1, wn = i >> 5 & 3, fr = i & 31;
+    const float* at = p.acc + (int64_t)tile * 65536 + (wn * 2 + wm) * 8192 + (h * 4 + j * 2 + ib) * 1024 + fr * 4;
+    for (int k = 0; k < pl.splits; k += 4) {
+        f32x4_t v[4][8];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                v[u][e] = k + u < pl.splits ? *reinterpret_cast<const f32x4_t*>(at + (int64_t)(k + u) * tiles * 65536 + (e >> 1) * 256 + (e & 1) * 128)
+                                            : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) s[e] += v[u][e];
+    }
+    T* out = dX + (int64_t)list[i] * p.D + d0;
 #pragma unroll
     for (int e = 0; e < 8; e += 2)
         if (d0 + e * 4 < p.D) {
@@ -707,9 +717,10 @@ int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks) {
     return launch_tiles(vocab_dx_kernel<parts_of<T>>, lim, blocks, s, p);
 }
 template <typename T>
-int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* place, int M, T* dX) {
+int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX) {
     ProfScope ps(K_REDUCE, s, (4.0 + sizeof(T)) * M * p.D);
-    hipLaunchKernelGGL(vocab_dx_rows_kernel<T>, dim3((M + 63) / 64, ((p.D + 31) / 32 + 3) / 4), dim3(256), 0, s, p, place, M, dX);
+    const int sums = (M + 63) / 64 * (((p.D + 31) / 32 + 3) / 4);
+    hipLaunchKernelGGL(vocab_dx_rows_kernel<T>, dim3((unsigned)(sums + (M + 15) / 16)), dim3(256), 0, s, p, list, place, M, sums, dX);
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
@@ -724,7 +735,7 @@ int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, b
 #define BOTH(T)                                                                                   \
     template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, int64_t);             \
     template int vocab_dx<T>(hipStream_t, const VocabGemm&, int64_t);                             \
-    template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, int, T*);            \
+    template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, const int*, int, T*); \
     template int vocab_dw<T>(hipStream_t, const VocabGemm&, void*, bool, bool, int64_t);
 BOTH(bf16)
 BOTH(float)

@@ -59,50 +59,58 @@ __global__ __launch_bounds__(256) void row_flags_kernel(const int* __restrict__ 
     if (lane == 0) flags[r] = (labels && in_vocab(labels[r], V) ? HAS_LABEL : 0) | (taught ? HAS_TEACHER : 0);
 }
 
-// One workgroup: list[i] = the i-th row that counts, place[r] = i or -1, zeros in the results of the others, and the plan.  Each
-// thread takes 16 rows at a time.
+// One workgroup: list[i] = the i-th row that counts, place[r] = i or -1, zeros in the results of the others, and the plan.  16384 rows
+// at a time, a wavefront 16 times 64 of them.  (Sixteen consecutive rows per thread: 28 us for 16384 rows.)
 __global__ __launch_bounds__(1024) void select_rows_kernel(const int* __restrict__ labels, const uint8_t* __restrict__ flags, int M, int V,
                                                            int* __restrict__ list, int* __restrict__ place, RowResults zero, PlanLimits lim,
                                                            VocabPlan* __restrict__ plan) {
-    __shared__ int wsum[16];
+    __shared__ unsigned long long masks[256];
+    __shared__ int before[256], wsum[4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     int base = 0;
     for (int r0 = 0; r0 < M; r0 += 16384) {
-        const int first = r0 + tid * 16;
-        unsigned mask = 0;
         int y[16];
 #pragma unroll
-        for (int k = 0; k < 16; ++k) y[k] = first + k < M ? flags ? flags[first + k] ? 0 : -1 : labels[first + k] : -1;
-#pragma unroll
-        for (int k = 0; k < 16; ++k) mask |= in_vocab(y[k], V) ? 1u << k : 0u;
-        int incl = __popc(mask);
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int t = __shfl_up(incl, o, 64);
-            if (lane >= o) incl += t;
-        }
-        if (lane == 63) wsum[wave] = incl;
-        __syncthreads();
-        int before = base, total = 0;
-        for (int w = 0; w < 16; ++w) {
-            if (w < wave) before += wsum[w];
-            total += wsum[w];
-        }
-        int i = before + incl - __popc(mask);
         for (int k = 0; k < 16; ++k) {
-            const int r = first + k;
+            const int r = r0 + k * 1024 + tid;
+            y[k] = r < M ? flags ? flags[r] ? 0 : -1 : labels[r] : -1;
+        }
+        unsigned long long mine[16];
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            mine[k] = __ballot(in_vocab(y[k], V));
+            if (lane == 0) masks[k * 16 + wave] = mine[k];
+        }
+        __syncthreads();
+        int n = 0, incl = 0;
+        if (tid < 256) {
+            n = incl = __popcll(masks[tid]);
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int t = __shfl_up(incl, o, 64);
+                if (lane >= o) incl += t;
+            }
+            if (lane == 63) wsum[wave] = incl;
+        }
+        __syncthreads();
+        if (tid < 256) before[tid] = base + incl - n + (wave > 0 ? wsum[0] : 0) + (wave > 1 ? wsum[1] : 0) + (wave > 2 ? wsum[2] : 0);
+        base += wsum[0] + wsum[1] + wsum[2] + wsum[3];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            const int r = r0 + k * 1024 + tid;
             if (r >= M) break;
-            const bool on = mask >> k & 1;
+            const bool on = mine[k] >> lane & 1;
+            const int i = before[k * 16 + wave] + __popcll(mine[k] & ((1ull << lane) - 1));
             place[r] = on ? i : -1;
             if (on) {
-                list[i++] = r;
+                list[i] = r;
             } else {
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     if (zero.p[q]) zero.p[q][r] = 0.f;
             }
         }
-        base += total;
         __syncthreads();
     }
     if (tid < 64) write_plan(base, V, lim, plan, tid);
@@ -545,8 +553,10 @@ static int vocab_check(const rev_vocab_cfg* c) {
 constexpr int FEW_ROWS = 128;
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
-// dz of a piece: 256 MB, what the memory-side cache holds, or 256 entries of all rows if that is more
-constexpr int64_t VOCAB_DZ_BYTES = 256 << 20;
+// dz of a piece: 512 MB, or 256 entries of all rows if that is more.  Loss and gradients of 8192 x 1024 to 131072 entries with 128, 256, 512
+// and 1024 MB: 8.31, 7.46, 7.34, 7.28 ms; 4096 x 768 to 50265 1.54, 1.50, 1.44, 1.45.  Fewer pieces have fuller rounds of tiles
+// and fewer passes over dx; that 256 MB would stay in the memory-side cache does not make up for them.
+constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 struct VocabLayout {
     int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, total;
     int64_t Mp, ldz;                 // ldz: float32 products
@@ -694,7 +704,7 @@ struct VocabRunner {
             if (dX) RC(vocab_dx<T>(s, g, L.lim.slots));
             if (dparams) RC(vocab_dw<T>(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
         }
-        return dX ? vocab_dx_rows<T>(s, g, v.place, M, dX) : REV_OK;
+        return dX ? vocab_dx_rows<T>(s, g, v.list, v.place, M, dX) : REV_OK;
     }
 
     // ---- float32 products ----
