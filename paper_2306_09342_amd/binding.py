@@ -447,8 +447,14 @@ def _vocab_common(cfg, params, X, workspace, floats=(), ints=()):
     return workspace
 
 
-def _vocab_stream(X, stream):
-    return ctypes.c_void_p((torch.cuda.current_stream(X.device) if stream is None else stream).cuda_stream)
+def _vocab_call(name, X, stream, *args):
+    """The entry point on the device of X, which need not be the current one, and on its current stream unless another is given."""
+    handle = ctypes.c_void_p((torch.cuda.current_stream(X.device) if stream is None else stream).cuda_stream)
+    if X.device.index == torch.cuda.current_device():
+        _check(getattr(lib(), name)(*args, handle))
+    else:
+        with torch.cuda.device(X.device):
+            _check(getattr(lib(), name)(*args, handle))
 
 
 def _vocab_out(out, name, shape, dtype, X):
@@ -474,9 +480,8 @@ def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=No
     """Softmax cross entropy of the rows of X over the vocabulary: {"loss", "lse"}, float32 [rows]; labels int32 [rows]."""
     ws = _vocab_common(cfg, params, X, workspace, ints=[(labels, (cfg.rows,))])
     loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X) for n in ("loss", "lse"))
-    with torch.cuda.device(X.device):
-        _check(lib().rev_xent_forward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(ws), ws.numel(),
-                                      _vocab_stream(X, stream)))
+    _vocab_call("rev_xent_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(ws),
+                ws.numel())
     return {"loss": loss, "lse": lse}
 
 
@@ -484,9 +489,8 @@ def rev_xent_backward(cfg, params, X, labels, lse, dloss, workspace=None, stream
     """Gradients of sum(dloss * loss), with the lse of the forward call: the members of `want`."""
     ws = _vocab_common(cfg, params, X, workspace, [(lse, (cfg.rows,)), (dloss, (cfg.rows,))], ints=[(labels, (cfg.rows,))])
     res = _vocab_grads(cfg, X, out, want)
-    with torch.cuda.device(X.device):
-        _check(lib().rev_xent_backward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(lse), _ptr(dloss), _ptr(res.get("dX")),
-                                       _ptr(res.get("dparams")), _ptr(ws), ws.numel(), _vocab_stream(X, stream)))
+    _vocab_call("rev_xent_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(lse), _ptr(dloss),
+                _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws), ws.numel())
     return res
 
 
@@ -498,10 +502,8 @@ def rev_distill_forward(cfg, params, X, teacher_idx, teacher_logits, labels=None
     res = {"loss": _vocab_out(out, "loss", (cfg.rows,), torch.float32, X), "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X)}
     if labels is not None:
         res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X)
-    with torch.cuda.device(X.device):
-        _check(lib().rev_distill_forward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx), _ptr(teacher_logits),
-                                         _ptr(res.get("loss_ce")), _ptr(res["loss"]), _ptr(res["lse"]), _ptr(ws), ws.numel(),
-                                         _vocab_stream(X, stream)))
+    _vocab_call("rev_distill_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
+                _ptr(teacher_logits), _ptr(res.get("loss_ce")), _ptr(res["loss"]), _ptr(res["lse"]), _ptr(ws), ws.numel())
     return res
 
 
@@ -512,10 +514,9 @@ def rev_distill_backward(cfg, params, X, teacher_idx, teacher_logits, lse, dloss
     ws = _vocab_common(cfg, params, X, workspace, [(teacher_logits, top), (lse, (2, cfg.rows)), (dloss, row), (dloss_ce, row)],
                        ints=[(labels, row), (teacher_idx, top)])
     res = _vocab_grads(cfg, X, out, want)
-    with torch.cuda.device(X.device):
-        _check(lib().rev_distill_backward(ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx), _ptr(teacher_logits),
-                                          _ptr(lse), _ptr(dloss_ce), _ptr(dloss), _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws),
-                                          ws.numel(), _vocab_stream(X, stream)))
+    _vocab_call("rev_distill_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
+                _ptr(teacher_logits), _ptr(lse), _ptr(dloss_ce), _ptr(dloss), _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws),
+                ws.numel())
     return res
 
 

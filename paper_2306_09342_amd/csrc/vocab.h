@@ -60,9 +60,8 @@ __device__ __forceinline__ void split3(float x, bf16 (&p)[3]) {
 }
 // T: bf16 (one part) or float (three)
 template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks);
-template <typename T> int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks);
+template <typename T> int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db);
 template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX);
-template <typename T> int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks);
 
 // Logits of few rows (vocab_few.hip): their statistics, or dz of the whole vocabulary.
 template <typename T> struct FewRows {

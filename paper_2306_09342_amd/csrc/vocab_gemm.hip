@@ -469,14 +469,13 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
 // dx of 256 rows and 256 columns over a range of a piece of the vocabulary, in float32, to a place of the range's own, in the order of
 // the accumulators (vocab_dx_rows_kernel reads it); later pieces add to it.
 template <int P>
-__global__ __launch_bounds__(512, 2) void vocab_dx_kernel(VocabGemm p) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+__device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem, int block) {
     const TileLane t;
     const VocabPlan pl = *p.plan;
     const int tiles_d = (p.D + 255) >> 8, tiles = __builtin_amdgcn_readfirstlane((pl.rows >> 8) * tiles_d);
     const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
-    if (n <= 0 || (int)blockIdx.x >= tiles * pl.splits) return;
-    const int lin = xcd_remap(blockIdx.x, tiles * pl.splits);
+    if (n <= 0 || block >= tiles * pl.splits) return;
+    const int lin = xcd_remap(block, tiles * pl.splits);
     const int split = __builtin_amdgcn_readfirstlane(lin / tiles), tile = __builtin_amdgcn_readfirstlane(lin - split * tiles);
     const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
     const int st0 = split * __builtin_amdgcn_readfirstlane(pl.stages), nst = min(__builtin_amdgcn_readfirstlane(pl.stages), ((n + 127) >> 7) * 2 - st0);
@@ -590,16 +589,15 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const i
 // dW of 256 entries of a piece and 256 columns over all rows, and, in the workgroups behind the tiles, db of 256 entries each: these
 // find the CUs that the last round of tiles leaves idle.
 template <typename TG, int P>
-__global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dparams, int db) {
-    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+__device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem, TG* dparams, int db, int block) {
     const TileLane t;
     const VocabPlan pl = *p.plan;
     const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
     if (n <= 0) return;
     const int tiles_v = (n + 255) >> 8, tiles_d = (p.D + 255) >> 8, tiles = tiles_v * tiles_d;
     const int64_t ldz = width;
-    if ((int)blockIdx.x >= tiles) {
-        const int b = blockIdx.x - tiles;
+    if (block >= tiles) {
+        const int b = block - tiles;
         if (!db || b >= tiles_v) return;
         const int c = threadIdx.x & 31, lane_row = threadIdx.x >> 5;
         float s[8] = {};
@@ -631,7 +629,7 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
         }
         return;
     }
-    const int tile = xcd_remap(blockIdx.x, tiles);
+    const int tile = xcd_remap(block, tiles);
     const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
     const int nst = __builtin_amdgcn_readfirstlane(((pl.count + 127) >> 7) * 2);
     f32x16_t acc[2][2][2];
@@ -690,6 +688,16 @@ __global__ __launch_bounds__(512, 2) void vocab_dw_kernel(VocabGemm p, TG* dpara
     }
 }
 
+// Both, which need dz alone: the first dx_blocks workgroups take dx, whose ranges are the longer ones, and dW's tiles fill the CUs
+// as these end.
+template <typename TG, int P>
+__global__ __launch_bounds__(512, 2) void vocab_grads_kernel(VocabGemm p, int dx_blocks, TG* dparams, int db) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int block = blockIdx.x;
+    if (block < dx_blocks) dx_block<P>(p, smem, block);
+    else dw_block<TG, P>(p, smem, dparams, db, block - dx_blocks);
+}
+
 template <typename... A>
 static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipStream_t s, A... args) {
     constexpr int lds = VG_LDS + 8 * VG_SIDE;
@@ -711,12 +719,6 @@ int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_
     return dual ? launch_tiles(vocab_logits_kernel<false, true, P>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false, P>, lim[3], blocks, s, p);
 }
 template <typename T>
-int vocab_dx(hipStream_t s, const VocabGemm& p, int64_t blocks) {
-    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
-    static LdsLimit lim;
-    return launch_tiles(vocab_dx_kernel<parts_of<T>>, lim, blocks, s, p);
-}
-template <typename T>
 int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX) {
     ProfScope ps(K_REDUCE, s, (4.0 + sizeof(T)) * M * p.D);
     const int sums = (M + 63) / 64 * (((p.D + 31) / 32 + 3) / 4);
@@ -724,19 +726,20 @@ int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int*
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
+// dx_blocks, dw_blocks: multiples of 8, most that there may be; 0: not wanted
 template <typename T>
-int vocab_dw(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, bool db, int64_t blocks) {
-    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D * ((dx_blocks > 0) + (dw_blocks > 0)));
     static LdsLimit lim[2];
+    const int first = (int)dx_blocks;
     if constexpr (sizeof(T) == 2)
-        if (grad_bf16) return launch_tiles(vocab_dw_kernel<bf16, 1>, lim[0], blocks, s, p, (bf16*)dparams, (int)db);
-    return launch_tiles(vocab_dw_kernel<float, parts_of<T>>, lim[1], blocks, s, p, (float*)dparams, (int)db);
+        if (grad_bf16) return launch_tiles(vocab_grads_kernel<bf16, 1>, lim[0], dx_blocks + dw_blocks, s, p, first, (bf16*)dparams, (int)db);
+    return launch_tiles(vocab_grads_kernel<float, parts_of<T>>, lim[1], dx_blocks + dw_blocks, s, p, first, (float*)dparams, (int)db);
 }
 #define BOTH(T)                                                                                   \
     template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, int64_t);             \
-    template int vocab_dx<T>(hipStream_t, const VocabGemm&, int64_t);                             \
-    template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, const int*, int, T*); \
-    template int vocab_dw<T>(hipStream_t, const VocabGemm&, void*, bool, bool, int64_t);
+    template int vocab_grads<T>(hipStream_t, const VocabGemm&, int64_t, int64_t, void*, bool, bool); \
+    template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, const int*, int, T*);
 BOTH(bf16)
 BOTH(float)
 #undef BOTH

@@ -701,8 +701,8 @@ struct VocabRunner {
             else RC(vocab_logits<T>(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
             if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
                               (int64_t)0, L.lim.dz);
-            if (dX) RC(vocab_dx<T>(s, g, L.lim.slots));
-            if (dparams) RC(vocab_dw<T>(s, g, dparams, c.grad_mode == REV_MODE_BF16, c.bias, tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0))));
+            RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) : 0, dparams,
+                              c.grad_mode == REV_MODE_BF16, c.bias));
         }
         return dX ? vocab_dx_rows<T>(s, g, v.list, v.place, M, dX) : REV_OK;
     }
