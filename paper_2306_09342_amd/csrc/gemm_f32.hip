@@ -286,12 +286,10 @@ static int launch_f32(hipStream_t s, const float* A, int64_t lda, const float* B
     return REV_OK;
 }
 
-// A contraction along which only A lies (B [K, N]) may have any length: A's rows are then read up to the next multiple of 4, which lda
-// holds, and what is there is multiplied by zeros (it has to be finite).
-static int check_gemm_f32(const float* A, int64_t lda, const float* B, int64_t ldb, int N, int K, const Epi& epi, bool any_k = false) {
+static int check_gemm_f32(const float* A, int64_t lda, const float* B, int64_t ldb, int N, int K, const Epi& epi) {
     const uintptr_t ptrs = (uintptr_t)A | (uintptr_t)B | (uintptr_t)epi.out | (uintptr_t)epi.out2 | (uintptr_t)epi.outf |
                            (uintptr_t)epi.bias | (uintptr_t)epi.res | (uintptr_t)epi.aux | (uintptr_t)epi.colsum;
-    if ((any_k ? lda < K : K % 4 != 0) || N % 4 || (lda & 3) || (ldb & 3) || epi.ldo % 4 || (ptrs & 15)) {
+    if (K % 4 || N % 4 || (lda & 3) || (ldb & 3) || epi.ldo % 4 || (ptrs & 15)) {
         set_error("gemm_f32: sizes must be multiples of 4 and every buffer 16-byte aligned");
         return REV_EINVAL;
     }
@@ -300,7 +298,7 @@ static int check_gemm_f32(const float* A, int64_t lda, const float* B, int64_t l
 
 template <bool BKM>
 static int gemm_f32(hipStream_t s, const float* A, int64_t lda, const float* B, int64_t ldb, int M, int N, int K, const Epi& epi) {
-    if (int rc = check_gemm_f32(A, lda, B, ldb, N, K, epi, BKM)) return rc;
+    if (int rc = check_gemm_f32(A, lda, B, ldb, N, K, epi)) return rc;
     ProfScope ps(K_GEMM_NT, s, 2.0 * M * N * K);
     const bool wide = f32_wide(M, N);
     switch (epi.kind) {

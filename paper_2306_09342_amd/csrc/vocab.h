@@ -59,25 +59,30 @@ __device__ __forceinline__ void split3(float x, bf16 (&p)[3]) {
     p[2] = from_f<bf16>(rest - to_f(p[1]));
 }
 // T: bf16 (one part) or float (three)
-template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks);
+// mid: tiles of 128 instead of 256; blocks: most of the latter
+template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, bool mid, int64_t blocks);
 template <typename T> int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db);
 template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX);
 
-// Logits of few rows (vocab_few.hip): their statistics, or dz of the whole vocabulary.
+// Few rows (vocab_few.hip): the statistics of the logits, or dz of the whole vocabulary in float32, and the gradients from that.
 template <typename T> struct FewRows {
     const VocabPlan* plan;
-    const T* x;                     // rows that count, [rows_x, Dp]
+    const T* x;                     // rows that count, [rows_x, Dp], zeros behind them
     const T* w;                     // [V, D]
     const T* bias;                  // [V] or null
     float* stats;                   // as VocabGemm::stats, of strips of 64 entries: row i at i stat_row, kinds stat_kind apart
     const float4* coef;
     const LabelDz* label_dz;
-    T* dz;                          // [rows_out, ldz], zeros behind the rows that count and the vocabulary; ldz = 0: the plan's width
+    float* dz;                      // [rows, ldz], zeros behind the rows that count
+    float* parts;                   // dx of a range of the vocabulary, [range][rows][D]
     int64_t stat_row, stat_kind, ldz;
-    int V, D, Dp, losses, rows_x, rows_out, blocks_m;
+    int V, D, Dp, losses, rows_x, rows, blocks_m;    // rows: most that count
+    int range, ranges, col_groups;  // entries per range, a multiple of 32
     float inv_tau;
 };
-// rows: most that count; width: columns that the launch covers
-template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual, int rows, int64_t width);
+template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual);
+template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, void* dparams, bool grad_bf16, bool db);
+template <typename T> int few_dx_rows(hipStream_t s, const FewRows<T>& p, const int* place, T* dX);
+void few_ranges(int rows, int V, int D, int es, int* range, int* ranges, int* col_groups);
 
 }  // namespace rev

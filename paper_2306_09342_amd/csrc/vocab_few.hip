@@ -9,6 +9,7 @@
 // What bounds it: reading W.
 #include "mfma.h"
 #include "vocab.h"
+#include <algorithm>
 
 namespace rev {
 
@@ -153,8 +154,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
             c = p.coef[i];
             if (p.label_dz) y = p.label_dz[i];
         }
-        const int64_t ldz = p.ldz ? p.ldz : pl.width;
-        T* out = p.dz + i * ldz + c0;
+        float* out = p.dz + i * p.ldz + c0;
         float d[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -163,24 +163,174 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
         }
 #pragma unroll
         for (int e = 0; e < EPT; e += 4)
-            if (c0 + e < ldz && i < p.rows_out) {
-                if constexpr (sizeof(T) == 4) {
-                    *reinterpret_cast<f32x4_t*>(out + e) = f32x4_t{d[e], d[e + 1], d[e + 2], d[e + 3]};
-                } else {
-                    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-                    *reinterpret_cast<bf16x4*>(out + e) = bf16x4{(__bf16)d[e], (__bf16)d[e + 1], (__bf16)d[e + 2], (__bf16)d[e + 3]};
-                }
-            }
+            if (c0 + e < p.ldz && i < p.rows) *reinterpret_cast<f32x4_t*>(out + e) = f32x4_t{d[e], d[e + 1], d[e + 2], d[e + 3]};
     }
 }
 
-template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual, int rows, int64_t width) {
-    ProfScope ps(K_VOCAB, s, 2.0 * rows * p.V * p.D);
+// The gradients of a range of the vocabulary and a group of columns from dz in float32, on the float32 matrix cores, so that dz is not
+// rounded again:  dW[v, d] = sum over i of dz[i, v] x[i, d]  of the range's entries, and dx[i, d] = sum over the range of dz[i, v]
+// W[v, d], to be added to the other ranges'.  The workgroup keeps the range's dz in LDS, where both products find their first
+// operand; the second, rows of W and x, is read from memory as it lies, 128 bytes of two rows at a time (bf16: as pairs of columns,
+// the two products of a pair one after the other).
+//
+// What bounds it: writing dW and reading W, and from about 32 rows on the float32 matrix cores.
+template <typename T, typename TG, int MB>
+__global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db) {
+    constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
+    extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1]
+    const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int count = __builtin_amdgcn_readfirstlane(p.plan->count);
+    const int r = blockIdx.x / p.col_groups, cg = blockIdx.x - r * p.col_groups, P = p.range + 1;
+    const int v0 = r * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
+    for (int i = wave; i < rows32; i += 4)
+        for (int c = lane; c < p.range; c += 64) dzs[i * P + c] = i < count && c < nv ? p.dz[i * p.ldz + v0 + c] : 0.f;
+    __syncthreads();
+    if (db && dparams && cg == 0)
+        for (int c = threadIdx.x; c < nv; c += 256) {
+            float s = 0.f;
+            for (int i = 0; i < count; ++i) s += dzs[i * P + c];
+            dparams[(int64_t)p.V * p.D + v0 + c] = from_f<TG>(s);
+        }
+    const int blocks = (p.D + COLS - 1) / COLS;
+    auto columns = [&](unsigned u, float (&f)[CS]) {
+        if constexpr (CS == 1) f[0] = __uint_as_float(u);
+        else { f[0] = __uint_as_float(u << 16); f[1] = __uint_as_float(u & 0xFFFF0000u); }
+    };
+    auto word = [&](const T* at) { return *reinterpret_cast<const unsigned*>(at); };
+    auto clear = [&](f32x16_t& c) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) c[v] = 0.f;
+    };
+    for (int b = cg * 4 + wave; b < blocks; b += 4 * p.col_groups) {
+        const int d = b * COLS + CS * fr, dc = min(d, p.D - CS);   // columns beyond D read the last ones again (never stored)
+        const T* x = p.x + dc;
+        const T* w = p.w + (int64_t)v0 * p.D + dc;
+        for (int vb = 0; vb < nv && dparams; vb += 32) {
+            f32x16_t acc[CS];
+#pragma unroll
+            for (int q = 0; q < CS; ++q) clear(acc[q]);
+            for (int s0 = 0; 2 * s0 < count; s0 += 8) {
+                unsigned xv[8];
+#pragma unroll
+                for (int s = 0; s < 8; ++s) xv[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.Dp);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    const int i = 2 * (s0 + s) + g;
+                    const float a = dzs[i * P + vb + fr];          // (rows up to whole 32 are there; 8 pairs divide them)
+                    float f[CS];
+                    columns(xv[s], f);
+#pragma unroll
+                    for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
+                }
+            }
+            if (d < p.D) {
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int n = vb + 8 * (v >> 2) + 4 * g + (v & 3);
+                    if (n >= nv) continue;
+                    TG* out = dparams + (int64_t)(v0 + n) * p.D + d;
+                    if constexpr (CS == 1) {
+                        *out = from_f<TG>(acc[0][v]);
+                    } else if constexpr (sizeof(TG) == 2) {
+                        typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+                        *reinterpret_cast<bf16x2_t*>(out) = bf16x2_t{(__bf16)acc[0][v], (__bf16)acc[1][v]};
+                    } else {
+                        *reinterpret_cast<float2*>(out) = make_float2(acc[0][v], acc[1][v]);
+                    }
+                }
+            }
+        }
+        for (int m0 = 0; m0 < rows32 && want_dx; m0 += 32 * MB) {
+            f32x16_t acc[MB][CS];
+#pragma unroll
+            for (int m = 0; m < MB; ++m)
+#pragma unroll
+                for (int q = 0; q < CS; ++q) clear(acc[m][q]);
+            for (int vb = 0; vb < nv; vb += 16) {
+                unsigned wv[8];
+#pragma unroll
+                for (int s = 0; s < 8; ++s) wv[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
+#pragma unroll
+                for (int s = 0; s < 8; ++s) {
+                    float f[CS];
+                    columns(wv[s], f);
+#pragma unroll
+                    for (int m = 0; m < MB; ++m) {
+                        const int i = min(m0 + m * 32, rows32 - 32) + fr;    // blocks beyond the last repeat it (not stored)
+                        const float a = dzs[i * P + vb + 2 * s + g];
+#pragma unroll
+                        for (int q = 0; q < CS; ++q) acc[m][q] = mfma_f32(a, f[q], acc[m][q]);
+                    }
+                }
+            }
+            if (d < p.D) {
+#pragma unroll
+                for (int m = 0; m < MB; ++m)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int i = m0 + m * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
+                        if (i >= count) continue;
+                        float* out = p.parts + ((int64_t)r * p.rows + i) * p.D + d;
+                        if constexpr (CS == 1) *out = acc[m][0][v];
+                        else *reinterpret_cast<float2*>(out) = make_float2(acc[m][0][v], acc[m][1][v]);
+                    }
+            }
+        }
+    }
+}
+
+// dX[r], 64 columns per workgroup: a sixteenth of the ranges per group of 16 lanes, added in order; zeros for a row that does not count.
+template <typename T>
+__global__ __launch_bounds__(256) void few_dx_rows_kernel(FewRows<T> p, const int* __restrict__ place, T* __restrict__ dX) {
+    __shared__ f32x4_t sh[16][16];
+    const int r = blockIdx.x, i = place[r], q = threadIdx.x & 15, k = threadIdx.x >> 4, d = blockIdx.y * 64 + q * 4;
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    if (i >= 0 && d < p.D) {
+        const int per = (p.ranges + 15) >> 4, last = min(p.ranges, (k + 1) * per);
+        const float* at = p.parts + (int64_t)i * p.D + d;
+        const int64_t step = (int64_t)p.rows * p.D;
+        for (int n = k * per; n < last; n += 8) {
+            f32x4_t v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = n + u < last ? *reinterpret_cast<const f32x4_t*>(at + (n + u) * step) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += v[u];
+        }
+    }
+    sh[k][q] = s;
+    __syncthreads();
+    if (k || d >= p.D) return;
+#pragma unroll
+    for (int n = 1; n < 16; ++n) s += sh[n][q];
+    T* out = dX + (int64_t)r * p.D + d;
+    if constexpr (sizeof(T) == 4) {
+        *reinterpret_cast<f32x4_t*>(out) = s;
+    } else {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        *reinterpret_cast<bf16x4*>(out) = bf16x4{(__bf16)s[0], (__bf16)s[1], (__bf16)s[2], (__bf16)s[3]};
+    }
+}
+
+// Ranges of the vocabulary and groups of columns: 256 to 512 workgroups where the sizes give as many, ranges of at most 256 entries (and
+// of fewer where their dz would not leave LDS for two workgroups).
+void few_ranges(int rows, int V, int D, int es, int* range, int* ranges, int* col_groups) {
+    const int blocks32 = (V + 31) / 32, rows32 = (rows + 31) / 32 * 32;
+    int per = (blocks32 + 255) / 256;
+    while (per > 1 && (per > 8 || rows32 * (per * 32 + 1) * 4 > 72 * 1024)) --per;
+    *range = per * 32;
+    *ranges = (blocks32 + per - 1) / per;
+    const int groups = ((D * es + 127) / 128 + 3) / 4;             // of four blocks of columns
+    *col_groups = std::max(1, std::min(groups, 512 / *ranges));
+}
+
+template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.rows * p.V * p.D);
     // 32 rows per workgroup instead of 64 as long as all of them run at once: the matrix cores of a CU then have half as much to do
-    const bool one = rows <= 32 || (int64_t)((rows + 31) / 32) * ((width + 63) / 64) <= 512;
-    const int covered = grad ? p.rows_out : rows;
-    p.blocks_m = (covered + (one ? 31 : 63)) / (one ? 32 : 64);
-    const dim3 grid((unsigned)(p.blocks_m * ((width + 63) / 64))), block(256);
+    const int tiles = (p.V + 63) / 64;
+    const bool one = p.rows <= 32 || (int64_t)((p.rows + 31) / 32) * tiles <= 512;
+    p.blocks_m = (p.rows + (one ? 31 : 63)) / (one ? 32 : 64);
+    const dim3 grid((unsigned)(p.blocks_m * tiles)), block(256);
 #define FEW1(G, U, MB) do {                                                                                          \
         static LdsLimit lim;                                                                                         \
         if (int rc = lim.ensure(reinterpret_cast<const void*>(few_logits_kernel<T, G, U, MB>), FewCfg<MB>::LDS)) return rc; \
@@ -195,7 +345,35 @@ template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, boo
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
-template int few_logits<bf16>(hipStream_t, FewRows<bf16>, bool, bool, int, int64_t);
-template int few_logits<float>(hipStream_t, FewRows<float>, bool, bool, int, int64_t);
+template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, void* dparams, bool grad_bf16, bool db) {
+    ProfScope ps(K_VOCAB, s, 2.0 * p.rows * p.V * p.D * (want_dx + (dparams != nullptr)));
+    const int rows32 = (p.rows + 31) / 32 * 32, lds = rows32 * (p.range + 1) * 4;
+    const dim3 grid((unsigned)(p.ranges * p.col_groups)), block(256);
+#define GRADS(TG, MB) do {                                                                                             \
+        static LdsLimit lim;                                                                                           \
+        if (int rc = lim.ensure(reinterpret_cast<const void*>(few_grads_kernel<T, TG, MB>), 160 * 1024)) return rc;    \
+        hipLaunchKernelGGL((few_grads_kernel<T, TG, MB>), grid, block, lds, s, p, (int)want_dx, (TG*)dparams, (int)db); \
+        REV_HIP(hipGetLastError());                                                                                    \
+        return REV_OK;                                                                                                 \
+    } while (0)
+    if constexpr (sizeof(T) == 2)
+        if (grad_bf16) { if (rows32 == 32) GRADS(bf16, 1); else GRADS(bf16, 2); }
+    if (rows32 == 32) GRADS(float, 1);
+    GRADS(float, 2);
+#undef GRADS
+}
+template <typename T> int few_dx_rows(hipStream_t s, const FewRows<T>& p, const int* place, T* dX) {
+    ProfScope ps(K_REDUCE, s, 4.0 * p.ranges * p.rows * p.D);
+    hipLaunchKernelGGL(few_dx_rows_kernel<T>, dim3(p.rows, (p.D + 63) / 64), dim3(256), 0, s, p, place, dX);
+    REV_HIP(hipGetLastError());
+    return REV_OK;
+}
+#define BOTH(T)                                                                       \
+    template int few_logits<T>(hipStream_t, FewRows<T>, bool, bool);                  \
+    template int few_grads<T>(hipStream_t, FewRows<T>, bool, void*, bool, bool);      \
+    template int few_dx_rows<T>(hipStream_t, const FewRows<T>&, const int*, T*);
+BOTH(bf16)
+BOTH(float)
+#undef BOTH
 
 }  // namespace rev

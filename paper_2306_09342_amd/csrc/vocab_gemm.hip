@@ -249,6 +249,78 @@ __device__ __forceinline__ void store_eights(bf16* out, const f32x16_t& d, bool 
     }
 }
 
+// Maximum of a row's logits (N blocks of 16 of each of the lanes g = 0, 1) and the sums of exp2((z - maximum) e) for one or two e.
+template <bool DUAL, int N>
+__device__ __forceinline__ void row_stats(const f32x16_t (&z)[N], float e0, float e1, float* out, int64_t kind, bool store) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) m = fmaxf(m, z[b][v]);
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int b = 0; b < N; ++b)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float d = z[b][v] - ref;                         // first: a lowest value times a scale may overflow
+            s0 += __builtin_amdgcn_exp2f(d * e0);
+            if (DUAL) s1 += __builtin_amdgcn_exp2f(d * e1);
+        }
+    s0 += __shfl_xor(s0, 32, 64);
+    if (DUAL) s1 += __shfl_xor(s1, 32, 64);
+    if (store) {
+        out[0] = m;
+        out[kind] = s0;
+        if (DUAL) out[2 * kind] = s1;
+    }
+}
+
+// dz of 16 entries of a row, those of lane g of 32, from its coefficients (without DUAL: the one exponential's; both losses have the
+// same at tau = 1), with the label's, entry `at` of the lane's, in its place; to `out`, where lane g's first eight of them go.
+template <bool DUAL, int P>
+__device__ __forceinline__ void dz_block(const f32x16_t& z, const float4& c, float rate0, float inv_tau, int at, float label_dz, bf16* out, int64_t part_dz) {
+    f32x16_t d;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        d[v] = c.x * __builtin_amdgcn_exp2f(fmaf(z[v], rate0, -c.y) * LOG2E);
+        if (DUAL) d[v] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z[v], inv_tau, -c.w) * LOG2E), d[v]);
+    }
+    if (__any((unsigned)at < 28u)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+            if (at == 8 * (v >> 2) + (v & 3)) d[v] = label_dz;
+    }
+#pragma unroll
+    for (int part = 0; part < P; ++part) {
+        store_eights(out + part * part_dz, d);
+        if (part + 1 < P)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float r = d[v] - to_f(from_f<bf16>(d[v]));
+                d[v] = fabsf(r) < INFINITY ? r : 0.f;
+            }
+    }
+    __builtin_amdgcn_sched_barrier(0);                             // one block's registers at a time
+}
+__device__ __forceinline__ float4 one_coef(float4 c, int losses) {
+    if (losses == LOSS_KD) { c.x = c.z; c.y = c.w; }
+    if (losses == (LOSS_CE | LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
+    return c;
+}
+// what replaces the accumulators' start at entry c0 + 8 (v / 4) + v % 4 of a tile that the vocabulary does not fill, or with biased
+// quads that it does not: -infinity beyond entry n, the bias from `from`
+template <int P>
+__device__ __forceinline__ void start_at_end(f32x16_t& z, int c0, int n, int part_quad, const void* from) {
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int c = 8 * (v >> 2) + (v & 3);
+        if (c >= n - c0) z[v] = -INFINITY;
+        else if (from && c >= part_quad - c0) z[v] = P == 1 ? to_f(reinterpret_cast<const bf16*>(from)[c0 + c]) : reinterpret_cast<const float*>(from)[c0 + c];
+    }
+}
+
 // The logits of tiles of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so
 // that neither costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the
 // sums are of exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are
@@ -345,19 +417,11 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
                     }
                 }
         if (n0 + 256 > n) {                                        // the vocabulary's or the piece's last tile
-            const int first = n0 + t.wm * 64 + 4 * t.g, beyond = n - first, part_quad = ((quad_end + 4) & ~3) - first;
-            const char* from = reinterpret_cast<const char*>(p.bias) + (int64_t)(v0 + first) * (P == 1 ? 2 : 4);
+            const char* from = biased ? reinterpret_cast<const char*>(p.bias) + (int64_t)v0 * (P == 1 ? 2 : 4) : nullptr;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int c = h * 128 + i * 32 + 8 * (v >> 2) + (v & 3);
-                        if (c >= beyond) acc[h][0][i][v] = -INFINITY;
-                        else if (biased && c >= part_quad)         // of a quad that the vocabulary does not fill
-                            acc[h][0][i][v] = P == 1 ? to_f(reinterpret_cast<const bf16*>(from)[c]) : reinterpret_cast<const float*>(from)[c];
-                    }
+                for (int i = 0; i < 2; ++i) start_at_end<P>(acc[h][0][i], n0 + h * 128 + t.wm * 64 + i * 32 + 4 * t.g, n, (quad_end + 4) & ~3, from);
         }
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -390,79 +454,152 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
 
         if constexpr (!GRAD) {
             const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
-            const int strip = (tn0 >> 7) + t.wm;
+            float* out = p.stats + (int64_t)((tn0 >> 7) + t.wm) * (DUAL ? 3 : 2) * p.Mp + tm0 + t.wn * 32 + t.fr;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float m = -INFINITY;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) m = fmaxf(m, acc[h][j][i][v]);
-                m = fmaxf(m, __shfl_xor(m, 32, 64));
-                const float ref = m == -INFINITY ? 0.f : m;
-                float s0 = 0.f, s1 = 0.f;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const float d = acc[h][j][i][v] - ref; // first: a lowest value times a scale may overflow
-                            s0 += __builtin_amdgcn_exp2f(d * e0);
-                            if (DUAL) s1 += __builtin_amdgcn_exp2f(d * e1);
-                        }
-                s0 += __shfl_xor(s0, 32, 64);
-                if (DUAL) s1 += __shfl_xor(s1, 32, 64);
-                if (t.g == 0) {
-                    float* out = p.stats + (int64_t)strip * (DUAL ? 3 : 2) * p.Mp + tm0 + j * 128 + t.wn * 32 + t.fr;
-                    out[0] = m;
-                    out[p.Mp] = s0;
-                    if (DUAL) out[2 * p.Mp] = s1;
-                }
+                const f32x16_t z[4] = {acc[0][j][0], acc[0][j][1], acc[1][j][0], acc[1][j][1]};
+                row_stats<DUAL>(z, e0, e1, out + j * 128, p.Mp, t.g == 0);
             }
         } else {
-            const int64_t ldz = width;
-            const float s0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
+            const float rate0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
+            const int dz_rows = (pl.count + 127) & ~127;           // dW goes over whole 128 rows
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int row = tm0 + j * 128 + t.wn * 32 + t.fr;
-                float4 c = tc[j];
-                if (!DUAL && (p.losses & LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
-                bf16* out = p.dz + row * ldz + tn0 + t.wm * 64 + 8 * t.g;
+                const float4 c = DUAL ? tc[j] : one_coef(tc[j], p.losses);
+                const int64_t row = tm0 + j * 128 + t.wn * 32 + t.fr;
+                if (row - t.fr >= dz_rows) continue;
+                bf16* out = p.dz + row * width + tn0 + t.wm * 64 + 8 * t.g;
+                const int at = ty[j].label - (v0 + tn0 + t.wm * 64 + 4 * t.g);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        f32x16_t d;
-#pragma unroll
-                        for (int v = 0; v < 16; ++v) {
-                            const float z = acc[h][j][i][v];
-                            d[v] = c.x * __builtin_amdgcn_exp2f(fmaf(z, s0, -c.y) * LOG2E);
-                            if (DUAL) d[v] = fmaf(c.z, __builtin_amdgcn_exp2f(fmaf(z, p.inv_tau, -c.w) * LOG2E), d[v]);
-                        }
-                        const int at = ty[j].label - (v0 + tn0 + h * 128 + t.wm * 64 + i * 32) - 4 * t.g;
-                        if (__any((unsigned)at < 28u)) {
-#pragma unroll
-                            for (int v = 0; v < 16; ++v)
-                                if (at == 8 * (v >> 2) + (v & 3)) d[v] = ty[j].dz;
-                        }
-#pragma unroll
-                        for (int part = 0; part < P; ++part) {
-                            store_eights(out + part * p.dz_part + h * 128 + i * 32, d);
-                            if (part + 1 < P)
-#pragma unroll
-                                for (int v = 0; v < 16; ++v) {
-                                    const float r = d[v] - to_f(from_f<bf16>(d[v]));
-                                    d[v] = fabsf(r) < INFINITY ? r : 0.f;
-                                }
-                        }
-                        __builtin_amdgcn_sched_barrier(0);         // one block's registers at a time
-                    }
+                    for (int i = 0; i < 2; ++i)
+                        dz_block<DUAL, P>(acc[h][j][i], c, rate0, p.inv_tau, at - h * 128 - i * 32, ty[j].dz, out + h * 128 + i * 32, p.dz_part);
             }
         }
         if (!more) break;
+    }
+}
+
+// The same in tiles of 128 rows and 128 entries, a workgroup of four wavefronts each, two on a CU, for launches that have too few of the
+// large ones (mid_tiles_pay, vocab_loss.hip).  Both operands of a stage of 64 travel through two stages of LDS; a stage is read as
+// a whole, asked for again and then multiplied.
+constexpr int VM_STAGE = 32768, VM_LDS = 2 * VM_STAGE;
+template <bool GRAD, bool DUAL, int P>
+__global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
+    extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
+    const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
+    const VocabPlan pl = *p.plan;
+    const int rows_m = __builtin_amdgcn_readfirstlane((pl.count + 127) >> 7);
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.V, v0 = GRAD ? width * p.piece : 0, n = min(width, p.V - v0);
+    const int tiles_n = n > 0 ? GRAD ? (n + 255) / 256 * 2 : (n + 127) >> 7 : 0, tiles = rows_m * tiles_n;    // dz is whole tiles of 256
+    if ((int)blockIdx.x >= tiles) return;
+    const int tile = xcd_remap(blockIdx.x, tiles), gn = tiles_n <= 8 ? tiles_n : 8, per_group = gn * rows_m, tg = tile / per_group;
+    const int in_grp = tile - tg * per_group, gw = min(gn, tiles_n - tg * gn);
+    const int m0 = __builtin_amdgcn_readfirstlane((in_grp / gw) * 128), n0 = __builtin_amdgcn_readfirstlane((tg * gn + in_grp % gw) * 128);
+
+    f32x16_t acc[2][2];                                            // [32-entry block of B][32-row block of A]
+    const bool biased = p.bias != nullptr;
+    const int es = P == 1 ? 2 : 4;
+    const char* bias = biased ? reinterpret_cast<const char*>(p.bias) + (int64_t)v0 * es : nullptr;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int c0 = n0 + wm * 64 + i * 32 + 4 * g;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            f32x4_t b = {0.f, 0.f, 0.f, 0.f};
+            if (biased && c0 + 8 * k + 4 <= p.V - v0) {
+                if (P == 1) {
+                    const u32x2_t u = *reinterpret_cast<const u32x2_t*>(bias + (c0 + 8 * k) * 2);
+                    b = f32x4_t{__uint_as_float(u[0] << 16), __uint_as_float(u[0] & 0xFFFF0000u), __uint_as_float(u[1] << 16), __uint_as_float(u[1] & 0xFFFF0000u)};
+                } else {
+                    b = *reinterpret_cast<const f32x4_t*>(bias + (c0 + 8 * k) * 4);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i][0][4 * k + e] = b[e];
+        }
+        if (n0 + 128 > n) start_at_end<P>(acc[i][0], c0, n, (p.V - v0) & ~3, bias);
+        acc[i][1] = acc[i][0];
+    }
+    if (m0 < pl.count && n0 < n) {
+        // a wavefront-wide load takes 8 rows of 8 chunks; four per operand and wavefront, 32 rows apart
+        const int row = wave * 8 + (lane >> 3), ch = ((lane & 7) ^ ((row >> 1) & 7)) << 4;
+        const int64_t ld = p.Dp;
+        const char* a_base = reinterpret_cast<const char*>(p.x + m0 * ld);
+        const char* b_base = reinterpret_cast<const char*>(p.wp + (int64_t)(v0 + n0) * ld);
+        const unsigned va = (unsigned)(row * ld * 2 + ch);
+        unsigned vb[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) vb[q] = (unsigned)(min(q * 32 + row, n - 1 - n0) * ld * 2 + ch);
+        const Parts<P> parts{p.Dp >> 6};
+        const int64_t part_a = p.Mp * ld * 2, part_b = p.V * ld * 2;
+        const unsigned lds0 = (unsigned)(uintptr_t)LDS_PTR(unsigned char, smem);
+        auto issue = [&](int kt) {
+            const int term = parts.term(kt);
+            const char* a = a_base + parts.a(term) * part_a + parts.within(kt, term) * 128;
+            const char* b = b_base + parts.b(term) * part_b + parts.within(kt, term) * 128;
+            const unsigned at = lds0 + (kt & 1) * VM_STAGE + wave * 1024;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) dma16_sbase(b, vb[q], at + q * 4096);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) dma16_sbase(a + q * 64 * ld, va, at + 16384 + q * 4096);
+        };
+        const int nst = parts.total();
+        issue(0);
+        issue(1);
+        for (int kt = 0; kt < nst; ++kt) {
+            if (kt + 1 < nst) wait_vm<8>();
+            else wait_vm<0>();
+            __builtin_amdgcn_s_barrier();                          // everybody's loads of this stage have landed
+            const unsigned char* at = smem + (kt & 1) * VM_STAGE;
+            bf16x8_t bf[4][2], af[4][2];
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                const int koff = ((2 * kk + g) ^ ((fr >> 1) & 7)) << 4;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    bf[kk][i] = *reinterpret_cast<const bf16x8_t*>(at + (wm * 64 + i * 32 + fr) * 128 + koff);
+                    af[kk][i] = *reinterpret_cast<const bf16x8_t*>(at + 16384 + (wn * 64 + i * 32 + fr) * 128 + koff);
+                }
+            }
+            wait_lds();
+            __builtin_amdgcn_s_barrier();                          // and has been read
+            if (kt + 2 < nst) issue(kt + 2);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[i][j] = mfma32(bf[kk][i], af[kk][j], acc[i][j]);
+        }
+    }
+    if constexpr (!GRAD) {
+        const float e1 = p.inv_tau * LOG2E, e0 = !DUAL && p.losses == LOSS_KD ? e1 : LOG2E;
+        float* out = p.stats + (int64_t)((n0 >> 6) + wm) * (DUAL ? 3 : 2) * p.Mp + m0 + wn * 64 + fr;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const f32x16_t z[2] = {acc[0][j], acc[1][j]};
+            row_stats<DUAL>(z, e0, e1, out + j * 32, p.Mp, g == 0);
+        }
+    } else {
+        const float rate0 = !DUAL && p.losses == LOSS_KD ? p.inv_tau : 1.f;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int64_t row = m0 + wn * 64 + j * 32 + fr;
+            float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);  // rows behind the last one that counts: 0 exp(z - infinity)
+            LabelDz y = {-1, 0.f};
+            if (row < pl.count) {
+                c = p.coef[row];
+                if (p.label_dz) y = p.label_dz[row];
+            }
+            if (!DUAL) c = one_coef(c, p.losses);
+            bf16* out = p.dz + row * width + n0 + wm * 64 + 8 * g;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                dz_block<DUAL, P>(acc[i][j], c, rate0, p.inv_tau, y.label - (v0 + n0 + wm * 64 + 4 * g) - i * 32, y.dz, out + i * 32, p.dz_part);
+        }
     }
 }
 
@@ -484,7 +621,12 @@ __device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem
     clear(acc);
     if (nst > 0) {
         const int64_t lda = width, ldb = p.ldw;
-        const unsigned va = (unsigned)(t.row_along() * lda * 2 + t.byte_along());
+        // rows of dz behind the last one that counts read that one again, their dx is not stored
+        unsigned va[2][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) va[h][q] = (unsigned)(min(h * 128 + q * 64 + t.row_along(), pl.count - 1 - m0) * lda * 2 + t.byte_along());
         const char* a_base = reinterpret_cast<const char*>(p.dz + m0 * lda + st0 * 64);
         const char* b_base = reinterpret_cast<const char*>(p.w + (int64_t)v0 * ldb + n0);
         unsigned col[2];                                           // columns beyond a row read its last eight again (never used)
@@ -495,9 +637,10 @@ __device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem
         const int64_t part_a = p.dz_part * 2, part_b = p.V * ldb * 2;
         auto issue_a = [&](auto half, int kt, unsigned lds) {
             const int term = parts.term(kt);
-            const char* src = a_base + parts.a(term) * part_a + decltype(half)::value * 256 * lda + parts.within(kt, term) * 128;
-            dma16_sbase(src, va, lds);
-            dma16_sbase(src + 128 * lda, va, lds + 8192);
+            constexpr int h = decltype(half)::value;
+            const char* src = a_base + parts.a(term) * part_a + parts.within(kt, term) * 128;
+            dma16_sbase(src, va[h][0], lds);
+            dma16_sbase(src, va[h][1], lds + 8192);
         };
         auto issue_b = [&](auto half, int kt, unsigned lds) {
             constexpr int h = decltype(half)::value;
@@ -520,7 +663,8 @@ __device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j) {
+            if (m0 + j * 128 + t.wn * 32 >= pl.count) continue;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
@@ -531,6 +675,7 @@ __device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem
                     if (p.piece > 0) v += *at;
                     *at = v;
                 }
+        }
 }
 
 // dX of the rows that count, 32 columns per thread: the ranges' sums of the row's place added in order.  The workgroups behind `sums`
@@ -604,10 +749,10 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
 #pragma unroll
         for (int part = P - 1; part >= 0; --part) {
             const bf16* src = p.dz + part * p.dz_part + b * 256 + c * 8;
-            for (int r0 = lane_row; r0 < pl.count; r0 += 128) {    // eight rows in flight (rows behind the last hold zeros)
+            for (int r0 = lane_row; r0 < pl.count; r0 += 128) {    // eight rows in flight (up to whole 128 rows, zeros at the end)
                 u32x4_t v[8];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) v[u] = r0 + 16 * u < pl.rows ? *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz) : u32x4_t{};
+                for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz);
 #pragma unroll
                 for (int u = 0; u < 8; ++u)
 #pragma unroll
@@ -699,10 +844,9 @@ __global__ __launch_bounds__(512, 2) void vocab_grads_kernel(VocabGemm p, int dx
 }
 
 template <typename... A>
-static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipStream_t s, A... args) {
-    constexpr int lds = VG_LDS + 8 * VG_SIDE;
+static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, int threads, int lds, hipStream_t s, A... args) {
     if (int rc = lim.ensure(reinterpret_cast<const void*>(kern), lds)) return rc;
-    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(512), lds, s, args...);
+    hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(threads), lds, s, args...);
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
@@ -710,13 +854,17 @@ static int launch_tiles(void (*kern)(A...), LdsLimit& lim, int64_t blocks, hipSt
 template <typename T> constexpr int parts_of = sizeof(T) == 2 ? 1 : 3;
 
 template <typename T>
-int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, int64_t blocks) {
+int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, bool mid, int64_t blocks) {
     constexpr int P = parts_of<T>;
     ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
-    blocks = std::min<int64_t>(blocks, 256);                       // one per CU
-    static LdsLimit lim[4];
-    if (grad) return dual ? launch_tiles(vocab_logits_kernel<true, true, P>, lim[0], blocks, s, p) : launch_tiles(vocab_logits_kernel<true, false, P>, lim[1], blocks, s, p);
-    return dual ? launch_tiles(vocab_logits_kernel<false, true, P>, lim[2], blocks, s, p) : launch_tiles(vocab_logits_kernel<false, false, P>, lim[3], blocks, s, p);
+    const int64_t large = std::min<int64_t>(blocks, 256);          // one per CU
+#define FORM(G, U) if (grad == G && dual == U) {                                                                          \
+        static LdsLimit lim[2];                                                                                          \
+        return mid ? launch_tiles(vocab_logits_mid_kernel<G, U, P>, lim[0], 4 * blocks, 256, VM_LDS, s, p)               \
+                   : launch_tiles(vocab_logits_kernel<G, U, P>, lim[1], large, 512, VG_LDS + 8 * VG_SIDE, s, p); }
+    FORM(false, false) FORM(false, true) FORM(true, false) FORM(true, true)
+#undef FORM
+    return REV_OK;
 }
 template <typename T>
 int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX) {
@@ -733,11 +881,11 @@ int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw
     static LdsLimit lim[2];
     const int first = (int)dx_blocks;
     if constexpr (sizeof(T) == 2)
-        if (grad_bf16) return launch_tiles(vocab_grads_kernel<bf16, 1>, lim[0], dx_blocks + dw_blocks, s, p, first, (bf16*)dparams, (int)db);
-    return launch_tiles(vocab_grads_kernel<float, parts_of<T>>, lim[1], dx_blocks + dw_blocks, s, p, first, (float*)dparams, (int)db);
+        if (grad_bf16) return launch_tiles(vocab_grads_kernel<bf16, 1>, lim[0], dx_blocks + dw_blocks, 512, VG_LDS, s, p, first, (bf16*)dparams, (int)db);
+    return launch_tiles(vocab_grads_kernel<float, parts_of<T>>, lim[1], dx_blocks + dw_blocks, 512, VG_LDS, s, p, first, (float*)dparams, (int)db);
 }
 #define BOTH(T)                                                                                   \
-    template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, int64_t);             \
+    template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, bool, int64_t);       \
     template int vocab_grads<T>(hipStream_t, const VocabGemm&, int64_t, int64_t, void*, bool, bool); \
     template int vocab_dx_rows<T>(hipStream_t, const VocabGemm&, const int*, const int*, int, T*);
 BOTH(bf16)

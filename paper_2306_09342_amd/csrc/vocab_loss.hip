@@ -13,6 +13,7 @@
 #include "rowwise.h"
 #include "vocab.h"
 #include <algorithm>
+#include <cstdlib>
 
 namespace rev {
 
@@ -30,7 +31,8 @@ __device__ __forceinline__ void write_plan(int count, int V, const PlanLimits& l
         p.width = (int)((V + pieces - 1) / pieces + 255) / 256 * 256;
         const int tiles = p.rows / 256 * lim.tiles_d, pairs = p.width / 128, s = lane + 1;
         const int stages = (pairs + s - 1) / s * 2;
-        unsigned cost = s <= pairs && tiles * s <= lim.slots ? (unsigned)((tiles * s + 255) / 256) * (stages + 10) : ~0u;
+        // a range of a tile is read once more
+        unsigned cost = s <= pairs && tiles * s <= lim.slots ? (unsigned)((tiles * s + 255) / 256) * (stages + 10) * 2 + s : ~0u;
         unsigned best = cost;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) best = min(best, (unsigned)__shfl_xor((int)best, o, 64));
@@ -490,45 +492,6 @@ __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float
 }
 
 // ---------------------------------------------------------------------------------
-// few rows in float32
-// ---------------------------------------------------------------------------------
-// Column sums of dz: 64 columns per workgroup, 16 wavefronts over the rows.
-__global__ __launch_bounds__(1024) void db_kernel(const float* __restrict__ dz, int64_t ld, int n, const VocabPlan* __restrict__ plan, float* __restrict__ out) {
-    __shared__ float sh[16][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, c = blockIdx.x * 64 + lane, count = plan->count;
-    float s = 0.f;
-    if (c < n)
-        for (int i = w; i < count; i += 16) s += dz[(int64_t)i * ld + c];
-    sh[w][lane] = s;
-    __syncthreads();
-    if (w == 0 && c < n) {
-        for (int k = 1; k < 16; ++k) s += sh[k][lane];
-        out[c] = s;
-    }
-}
-// The last n < 4 rows of dW, which the product in fours leaves: out[v][d] = sum over i of dz[i][v] x[i][d].
-__global__ __launch_bounds__(256) void dw_rest_kernel(const float* __restrict__ dz, int64_t ld, const float* __restrict__ x, int D, int n,
-                                                      const VocabPlan* __restrict__ plan, float* __restrict__ out) {
-    const int c = blockIdx.x * 256 + threadIdx.x, e = c / D, d = c - e * D, count = plan->count;
-    if (e >= n) return;
-    float s = 0.f;
-    for (int i = 0; i < count; ++i) s = fmaf(dz[(int64_t)i * ld + e], x[(int64_t)i * D + d], s);
-    out[c] = s;
-}
-
-// dX[r] from the sums of its place, zeros for a row that does not count.
-__global__ __launch_bounds__(256) void dx_rows_kernel(const float* __restrict__ acc, const int* __restrict__ place, int M, int D, float* __restrict__ dX) {
-    const int per = D / 4;
-    const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (c >= (int64_t)M * per) return;
-    const int64_t r = c / per;
-    const int d = (int)(c - r * per) * 4, i = place[r];
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (i >= 0) v = load4(acc + (int64_t)i * D + d);
-    store4(dX + r * D + d, v);
-}
-
-// ---------------------------------------------------------------------------------
 // host side
 // ---------------------------------------------------------------------------------
 static int vocab_check(const rev_vocab_cfg* c) {
@@ -549,8 +512,24 @@ static int vocab_check(const rev_vocab_cfg* c) {
     return REV_OK;
 }
 
-// Up to FEW_ROWS rows the logits come from vocab_few.hip, and float32 takes the float32 products of the stack.
-constexpr int FEW_ROWS = 128;
+// The kernels of few rows (vocab_few.hip): TODO
+static int64_t few_blocks(int64_t M, int64_t V) { return (M + 63) / 64 * ((V + 63) / 64); }
+static bool few_forward(const rev_vocab_cfg& c) {
+    const char* e = getenv("VL_FF");
+    if (e) return atoi(e);
+    return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 400;
+}
+static bool few_backward(const rev_vocab_cfg& c) {
+    const char* e = getenv("VL_FB");
+    if (e) return atoi(e);
+    return c.rows <= 32 || (c.rows <= 512 && few_blocks(c.rows, c.vocab) <= 128);
+}
+// Tiles of 128 in the place of 256 for the logits, where the latter leave most CUs without one.
+static bool mid_tiles_pay(int64_t M, int64_t V) {
+    const char* e = getenv("VL_MID");
+    if (e) return atoi(e);
+    return (M + 255) / 256 * ((V + 255) / 256) <= 128;
+}
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // dz of a piece: 512 MB, or 256 entries of all rows if that is more.  Loss and gradients of 8192 x 1024 to 131072 entries with 128, 256, 512
@@ -558,21 +537,25 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // and fewer passes over dx; that 256 MB would stay in the memory-side cache does not make up for them.
 constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, total;
-    int64_t Mp, ldz;                 // ldz: float32 products
-    bool few;
-    int parts;                       // bf16 parts of an operand of the products; 0: float32 products (gemm_f32.hip)
+    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, dzf, parts_dx, total;
+    int64_t Mp, ldz;                 // ldz: of dz in float32
+    bool few_f, few_b, mid;          // few rows, forward and backward; tiles of 128
+    int parts;                       // bf16 parts of an operand of the products of tiles
     int Dp, strips, pieces;          // pieces: most that a plan may have
+    int range, ranges, col_groups;   // few_ranges
     PlanLimits lim;
 };
 static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     VocabLayout L = {};
     const int64_t M = c.rows, D = c.d_model, V = c.vocab;
-    L.few = M <= FEW_ROWS;
-    L.parts = c.mode == REV_MODE_BF16 ? 1 : L.few ? 0 : 3;
-    L.Dp = L.parts ? (int)up(D, 128) : c.d_model;
-    L.Mp = L.parts ? up(M, 256) : M;
-    L.strips = (int)(L.few ? (V + 63) / 64 : (V + 255) / 256 * 2);
+    L.few_f = few_forward(c);
+    L.few_b = few_backward(c);
+    L.parts = c.mode == REV_MODE_BF16 ? 1 : 3;
+    const int es = L.parts == 1 ? 2 : 4;
+    L.Dp = (int)up(D, 128);
+    L.Mp = up(M, 256);
+    L.mid = mid_tiles_pay(M, V);
+    L.strips = (int)(L.few_f ? (V + 63) / 64 : L.mid ? (V + 127) / 128 * 2 : (V + 255) / 256 * 2);
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
     L.plan = take(sizeof(VocabPlan));
@@ -582,23 +565,24 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.coef = take(16 * L.Mp);
     L.label_dz = take(8 * L.Mp);
     L.zs = take(4 * M * (c.top_k + 1));
-    L.stats = take(12 * (L.few ? M : L.Mp) * L.strips);
-    if (L.parts) {
+    L.stats = take(12 * (L.few_f ? M : L.Mp) * L.strips);
+    // the rows' copy: their own type, or parts of it, in the place of the larger
+    L.xc = take(L.Mp * L.Dp * (L.parts == 1 ? 2 : 6));
+    if (!L.few_f || !L.few_b) L.w = L.Dp != D || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
+    if (!L.few_b) {
         const int64_t all = L.Mp * up(V, 256);
-        L.lim.dz = L.few ? all : std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
+        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
         L.lim.tiles_d = (int)((D + 255) / 256);
         L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
         L.pieces = (int)((V + least - 1) / least);
-        L.xc = take(2 * L.parts * L.Mp * L.Dp);
-        L.w = (!L.few && L.Dp != D) || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
         L.dz = take(2 * L.parts * L.lim.dz);
         L.acc = take((int64_t)L.lim.slots * 65536 * 4);
     } else {
         L.ldz = up(V, 4);
-        L.xc = take(4 * M * D);
-        L.dz = take(4 * M * L.ldz);
-        L.acc = take(4 * M * D);
+        few_ranges(c.rows, c.vocab, c.d_model, es, &L.range, &L.ranges, &L.col_groups);
+        L.dzf = take(4 * M * L.ldz);
+        L.parts_dx = take(4 * (int64_t)L.ranges * M * D);
     }
     L.total = at;
     return L;
@@ -646,13 +630,11 @@ struct VocabRunner {
         LAUNCH((gather_kernel<T, P>), rows, block, v, g, flags());
         return REV_OK;
     }
-    int prepare(const void* X, const RowResults& zero, const Cotangents& cot) { return L.parts ? prepare<kParts>(X, zero, cot) : prepare<0>(X, zero, cot); }
-
     int join(const RowResults& out) {
         ProfScope ps(K_REDUCE, s, 12.0 * M * L.strips);
         const int64_t kind = L.strips;
-        if (L.few && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
-        else if (L.few) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
         else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
         else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
         return REV_OK;
@@ -660,11 +642,10 @@ struct VocabRunner {
     FewRows<T> few_args() {
         FewRows<T> f = {};
         f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
-        f.label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); f.dz = at<T>(L.dz);
+        f.label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
         f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
-        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.inv_tau = v.inv_tau;
-        f.rows_x = (int)L.Mp;
-        f.rows_out = L.parts ? (int)up(M, 128) : M;                // dw goes over whole 128 rows
+        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = M;
+        f.range = L.range; f.ranges = L.ranges; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
         return f;
     }
 
@@ -676,7 +657,7 @@ struct VocabRunner {
         g->Mp = L.Mp; g->dz_part = L.lim.dz; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
         g->w = g->wp = (const bf16*)params;
         g->ldw = D;
-        if (L.w) {
+        if (L.Dp != D || kParts > 1) {
             ProfScope ps(K_CONVERT, s, (sizeof(T) + 2.0 * kParts) * V * L.Dp);
             LAUNCH(lay_out_kernel<T>, blocks_of((int64_t)V * L.Dp * sizeof(T) / 16, 256), dim3(256), params, V, D, L.Dp, at<bf16>(L.w));
             g->wp = at<bf16>(L.w);
@@ -687,7 +668,7 @@ struct VocabRunner {
     int forward_parts(const RowResults& out) {
         VocabGemm g;
         RC(gemm_args(&g));
-        RC(vocab_logits<T>(s, g, false, dual(), L.Mp / 256 * ((V + 255) / 256)));
+        RC(vocab_logits<T>(s, g, false, dual(), L.mid, L.Mp / 256 * ((V + 255) / 256)));
         return join(out);
     }
     int backward_parts(T* dX, void* dparams) {
@@ -697,8 +678,7 @@ struct VocabRunner {
             // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
             const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
             g.piece = k;
-            if (L.few) RC(few_logits<T>(s, few_args(), true, false, M, up(V, 256)));
-            else RC(vocab_logits<T>(s, g, true, dual(), std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
+            RC(vocab_logits<T>(s, g, true, dual(), L.mid, std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
             if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
                               (int64_t)0, L.lim.dz);
             RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) : 0, dparams,
@@ -707,38 +687,31 @@ struct VocabRunner {
         return dX ? vocab_dx_rows<T>(s, g, v.list, v.place, M, dX) : REV_OK;
     }
 
-    // ---- float32 products ----
-    int backward_f32(float* dX, float* dparams) {
-        float *dz = at<float>(L.dz), *acc = at<float>(L.acc), *x = at<float>(L.xc);
-        const float* w = (const float*)params;
-        RC(few_logits<T>(s, few_args(), true, false, M, L.ldz));
-        if (v.idx) LAUNCH((sparse_dz_kernel<float, 0>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), 0, V, dz, L.ldz, (int64_t)0);
-        if (dX) {
-            Epi e = {}; e.kind = EPI_PLAIN_F32; e.outf = acc; e.ldo = D; e.solo = true;
-            RC(gemm_nn_f32(s, dz, L.ldz, w, D, M, D, V, e));
-            LAUNCH(dx_rows_kernel, blocks_of((int64_t)M * D / 4, 256), dim3(256), acc, v.place, M, D, dX);
-        }
-        if (dparams) {
-            const int whole = V / 4 * 4;
-            const WgradF32Item it = {dz, L.ldz, x, D, whole, D, dparams, nullptr};
-            if (whole) RC(gemm_wgrad_f32_group(s, &it, 1, M));
-            if (V > whole) LAUNCH(dw_rest_kernel, blocks_of((V - whole) * D, 256), dim3(256), dz + whole, L.ldz, x, D, V - whole, v.plan, dparams + (int64_t)whole * D);
-            if (c.bias) LAUNCH(db_kernel, blocks_of(V, 64), dim3(1024), dz, L.ldz, V, v.plan, dparams + (int64_t)V * D);
-        }
-        return REV_OK;
+    // ---- few rows ----
+    int backward_few(T* dX, void* dparams) {
+        const FewRows<T> f = few_args();
+        RC(few_logits<T>(s, f, true, false));
+        if (v.idx) LAUNCH((sparse_dz_kernel<float, 0>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), 0, V, f.dz, f.ldz, (int64_t)0);
+        RC(few_grads<T>(s, f, dX != nullptr, dparams, c.grad_mode == REV_MODE_BF16, c.bias));
+        return dX ? few_dx_rows<T>(s, f, v.place, dX) : REV_OK;
     }
 
     int forward(const void* X, const RowResults& out) {
-        RC(prepare(X, out, Cotangents{}));
-        if (!L.few) return forward_parts(out);
-        RC(few_logits<T>(s, few_args(), false, dual(), M, V));
+        if (!L.few_f) {
+            RC(prepare<kParts>(X, out, Cotangents{}));
+            return forward_parts(out);
+        }
+        RC(prepare<0>(X, out, Cotangents{}));
+        RC(few_logits<T>(s, few_args(), false, dual()));
         return join(out);
     }
     int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
-        RC(prepare(X, RowResults{}, cot));
-        if (L.parts) return backward_parts((T*)dX, dparams);
-        if constexpr (kParts == 3) return backward_f32((float*)dX, (float*)dparams);
-        return REV_OK;
+        if (!L.few_b) {
+            RC(prepare<kParts>(X, RowResults{}, cot));
+            return backward_parts((T*)dX, dparams);
+        }
+        RC(prepare<0>(X, RowResults{}, cot));
+        return backward_few((T*)dX, dparams);
     }
 };
 
