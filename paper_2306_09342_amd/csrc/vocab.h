@@ -73,10 +73,11 @@ template <typename T> struct FewRows {
     float* stats;                   // as VocabGemm::stats, of strips of 64 entries: row i at i stat_row, kinds stat_kind apart
     const float4* coef;
     const LabelDz* label_dz;
-    float* dz;                      // [rows, ldz], zeros behind the rows that count
+    float* dz;                      // [rows_out, ldz], zeros behind the rows that count and the vocabulary
+    bf16* tile_dz;                  // the same in bf16, for the products of tiles, in the plan's width; or null
     float* parts;                   // dx of a range of the vocabulary, [range][rows][D]
     int64_t stat_row, stat_kind, ldz;
-    int V, D, Dp, losses, rows_x, rows, blocks_m;    // rows: most that count
+    int V, D, Dp, losses, rows_x, rows, rows_out, blocks_m;    // rows: most that count
     int range, ranges, col_groups;  // entries per range, a multiple of 32
     float inv_tau;
 };

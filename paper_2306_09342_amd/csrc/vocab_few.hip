@@ -6,7 +6,7 @@
 // which the softmax statistics or dz are made of.  (Both operands read straight into registers instead: every lane of such a load is
 // in another row, and the address unit took 12 us for 64 rows and 1000 entries of 768, 31 for one row and 50265.)
 //
-// What bounds it: reading W.
+// What bounds it: reading W.  One row of 768, 50265 entries, bf16 (77 MB): 19 us, 4.1 TB/s; 16 rows of 1024 (103 MB): 22 us.
 #include "mfma.h"
 #include "vocab.h"
 #include <algorithm>
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
             c = p.coef[i];
             if (p.label_dz) y = p.label_dz[i];
         }
-        float* out = p.dz + i * p.ldz + c0;
+        const int64_t ldz = p.tile_dz ? pl.width : p.ldz;
         float d[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -162,8 +162,16 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
             if (c0 + e == y.label) d[e] = y.dz;
         }
 #pragma unroll
-        for (int e = 0; e < EPT; e += 4)
-            if (c0 + e < p.ldz && i < p.rows) *reinterpret_cast<f32x4_t*>(out + e) = f32x4_t{d[e], d[e + 1], d[e + 2], d[e + 3]};
+        for (int e = 0; e < EPT; e += 4) {
+            if (c0 + e >= ldz || i >= p.rows_out) continue;
+            const int64_t at = i * ldz + c0 + e;
+            if (sizeof(T) == 2 && p.tile_dz) {
+                typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+                *reinterpret_cast<bf16x4*>(p.tile_dz + at) = bf16x4{(__bf16)d[e], (__bf16)d[e + 1], (__bf16)d[e + 2], (__bf16)d[e + 3]};
+            } else {
+                *reinterpret_cast<f32x4_t*>(p.dz + at) = f32x4_t{d[e], d[e + 1], d[e + 2], d[e + 3]};
+            }
+        }
     }
 }
 
@@ -173,7 +181,8 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 // operand; the second, rows of W and x, is read from memory as it lies, 128 bytes of two rows at a time (bf16: as pairs of columns,
 // the two products of a pair one after the other).
 //
-// What bounds it: writing dW and reading W, and from about 32 rows on the float32 matrix cores.
+// What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
+// entries, float32: one row 58 us (5.3 TB/s of W and dW), 32 rows 102 us.
 template <typename T, typename TG, int MB>
 __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
@@ -206,22 +215,41 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
         const int d = b * COLS + CS * fr, dc = min(d, p.D - CS);   // columns beyond D read the last ones again (never stored)
         const T* x = p.x + dc;
         const T* w = p.w + (int64_t)v0 * p.D + dc;
+        // up to 32 rows of x stay in registers
+        constexpr int KEPT = MB == 1 ? 16 : 1;
+        unsigned kept[KEPT];
+        if (MB == 1 && dparams) {
+#pragma unroll
+            for (int s = 0; s < KEPT; ++s) kept[s] = 2 * s < count ? word(x + (int64_t)(2 * s + g) * p.Dp) : 0u;
+        }
         for (int vb = 0; vb < nv && dparams; vb += 32) {
             f32x16_t acc[CS];
 #pragma unroll
             for (int q = 0; q < CS; ++q) clear(acc[q]);
-            for (int s0 = 0; 2 * s0 < count; s0 += 8) {
-                unsigned xv[8];
+            auto add = [&](int s, unsigned u) {
+                const float a = dzs[(2 * s + g) * P + vb + fr];    // (rows up to whole 32 are there)
+                float f[CS];
+                columns(u, f);
 #pragma unroll
-                for (int s = 0; s < 8; ++s) xv[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.Dp);
+                for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
+            };
+            if constexpr (MB == 1) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
-                    const int i = 2 * (s0 + s) + g;
-                    const float a = dzs[i * P + vb + fr];          // (rows up to whole 32 are there; 8 pairs divide them)
-                    float f[CS];
-                    columns(xv[s], f);
+                for (int s = 0; s < KEPT; ++s)
+                    if (2 * s < count) add(s, kept[s]);
+            } else {
+                unsigned xv[8], next[8];
+                auto load = [&](unsigned (&to)[8], int s0) {
 #pragma unroll
-                    for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
+                    for (int s = 0; s < 8; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.Dp);
+                };
+                load(next, 0);
+                for (int s0 = 0; 2 * s0 < count; s0 += 8) {
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) xv[s] = next[s];
+                    load(next, s0 + 8);
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) add(s0 + s, xv[s]);
                 }
             }
             if (d < p.D) {
@@ -247,12 +275,18 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
             for (int m = 0; m < MB; ++m)
 #pragma unroll
                 for (int q = 0; q < CS; ++q) clear(acc[m][q]);
-            for (int vb = 0; vb < nv; vb += 16) {
-                unsigned wv[8];
+            unsigned wv[16], next[16];                             // 32 entries, asked for 32 ahead
+            auto load = [&](unsigned (&to)[16], int vb) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s) wv[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
+                for (int s = 0; s < 16; ++s) to[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
+            };
+            load(next, 0);
+            for (int vb = 0; vb < nv; vb += 32) {
 #pragma unroll
-                for (int s = 0; s < 8; ++s) {
+                for (int s = 0; s < 16; ++s) wv[s] = next[s];
+                load(next, vb + 32);
+#pragma unroll
+                for (int s = 0; s < 16; ++s) {
                     float f[CS];
                     columns(wv[s], f);
 #pragma unroll
@@ -312,24 +346,25 @@ __global__ __launch_bounds__(256) void few_dx_rows_kernel(FewRows<T> p, const in
     }
 }
 
-// Ranges of the vocabulary and groups of columns: 256 to 512 workgroups where the sizes give as many, ranges of at most 256 entries (and
-// of fewer where their dz would not leave LDS for two workgroups).
+// Ranges of the vocabulary and groups of columns: about 320 ranges, of at most 256 entries (of fewer where their dz would not leave LDS
+// for two workgroups), each by as many workgroups as it has groups of four column blocks.  32 rows of 768 to 50265 entries, loss and gradients
+// backward in us by entries per range and groups, bf16 / float32: 224, 2: 126 / 149; 224, 3: 121 / 143; 128, 3: 118 / 157; 64, 3: 129 / 178.
 void few_ranges(int rows, int V, int D, int es, int* range, int* ranges, int* col_groups) {
     const int blocks32 = (V + 31) / 32, rows32 = (rows + 31) / 32 * 32;
-    int per = (blocks32 + 255) / 256;
+    int per = (blocks32 + 319) / 320;
     while (per > 1 && (per > 8 || rows32 * (per * 32 + 1) * 4 > 72 * 1024)) --per;
     *range = per * 32;
     *ranges = (blocks32 + per - 1) / per;
     const int groups = ((D * es + 127) / 128 + 3) / 4;             // of four blocks of columns
-    *col_groups = std::max(1, std::min(groups, 512 / *ranges));
+    *col_groups = std::max(1, std::min(groups, 1024 / *ranges));
 }
 
 template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual) {
     ProfScope ps(K_VOCAB, s, 2.0 * p.rows * p.V * p.D);
     // 32 rows per workgroup instead of 64 as long as all of them run at once: the matrix cores of a CU then have half as much to do
-    const int tiles = (p.V + 63) / 64;
+    const int tiles = grad && p.tile_dz ? (p.V + 255) / 256 * 4 : (p.V + 63) / 64, covered = grad ? p.rows_out : p.rows;
     const bool one = p.rows <= 32 || (int64_t)((p.rows + 31) / 32) * tiles <= 512;
-    p.blocks_m = (p.rows + (one ? 31 : 63)) / (one ? 32 : 64);
+    p.blocks_m = (covered + (one ? 31 : 63)) / (one ? 32 : 64);
     const dim3 grid((unsigned)(p.blocks_m * tiles)), block(256);
 #define FEW1(G, U, MB) do {                                                                                          \
         static LdsLimit lim;                                                                                         \

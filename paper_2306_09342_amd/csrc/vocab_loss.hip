@@ -13,7 +13,6 @@
 #include "rowwise.h"
 #include "vocab.h"
 #include <algorithm>
-#include <cstdlib>
 
 namespace rev {
 
@@ -512,24 +511,28 @@ static int vocab_check(const rev_vocab_cfg* c) {
     return REV_OK;
 }
 
-// The kernels of few rows (vocab_few.hip): TODO
+// Where the kernels of few rows (vocab_few.hip) take the place of the products in tiles; blocks: of 64 rows and 64 entries.  us, tiles / few
+// rows, D = 768 unless said.
+// Forward, bf16: 1 row, V = 50265: 35 / 27; 64: 35 / 32; 96: 35 / 43; V = 10007, 128 rows (314 blocks): 22 / 19; 256 (628): 22 / 25; V = 1000, 512:
+// 22 / 18.  float32: 128 rows, V = 50265: 182 / 120; V = 10007: 76 / 45; 256 rows, 10007: 77 / 73; 512, V = 1000, D = 384: 41 / 18.
 static int64_t few_blocks(int64_t M, int64_t V) { return (M + 63) / 64 * ((V + 63) / 64); }
 static bool few_forward(const rev_vocab_cfg& c) {
-    const char* e = getenv("VL_FF");
-    if (e) return atoi(e);
     return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 400;
 }
+// Backward.  bf16: V = 50265, 1 row: 87 / 78, 16: 81 / 98; V = 131072, D = 256, 4 rows: 96 / 70; V = 10007, 16 rows: 41 / 35, 64: 43 / 56; V = 1000, 8: 32
+// / 22, 64: 33 / 34.  float32, whose tiles need W in parts first: V = 50265, 1 row: 359 / 118, 64: 376 / 261; V = 10007, 128: 151 / 123; V =
+// 1000, 256: 106 / 72, 512: 127 / 122; V = 2000, D = 1024, 300: 136 / 115.
 static bool few_backward(const rev_vocab_cfg& c) {
-    const char* e = getenv("VL_FB");
-    if (e) return atoi(e);
-    return c.rows <= 32 || (c.rows <= 512 && few_blocks(c.rows, c.vocab) <= 128);
+    const int64_t blocks = few_blocks(c.rows, c.vocab);
+    if (c.mode == REV_MODE_BF16) return c.rows <= 4 || (c.rows <= 32 && blocks <= 160);
+    return c.rows <= 64 || (c.rows <= 128 && c.vocab <= 16384) || (c.rows <= 512 && blocks <= 160);
 }
-// Tiles of 128 in the place of 256 for the logits, where the latter leave most CUs without one.
-static bool mid_tiles_pay(int64_t M, int64_t V) {
-    const char* e = getenv("VL_MID");
-    if (e) return atoi(e);
-    return (M + 255) / 256 * ((V + 255) / 256) <= 128;
-}
+// dz alone by them, the gradients in tiles (bf16).  V = 1000, 128 rows: 35 / 29, 512: 45 / 39; V = 10007, 128 rows: 54 / 53.
+static bool few_for_dz(const rev_vocab_cfg& c) { return c.mode == REV_MODE_BF16 && !few_backward(c) && few_blocks(c.rows, c.vocab) <= 160; }
+// Tiles of 128 in the place of 256 for the logits, where the latter leave half of the CUs without one.  Forward, us, 256 / 128: 256 rows, V =
+// 10007 (40 tiles of 256): 29 / 23; 512, D = 1280 (80): 41 / 35; 8192, V = 1000 (128): 44 / 37; 777, D = 256, V = 10007 (160): 24 / 25; 200, V =
+// 50265 (197): 38 / 51.  float32: 512, D = 1280 (80): 152 / 133; 1024, V = 10007 (160): 110 / 144.
+static bool mid_tiles_pay(int64_t M, int64_t V) { return (M + 255) / 256 * ((V + 255) / 256) <= 128; }
 
 static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // dz of a piece: 512 MB, or 256 entries of all rows if that is more.  Loss and gradients of 8192 x 1024 to 131072 entries with 128, 256, 512
@@ -539,7 +542,7 @@ constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 struct VocabLayout {
     int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, dzf, parts_dx, total;
     int64_t Mp, ldz;                 // ldz: of dz in float32
-    bool few_f, few_b, mid;          // few rows, forward and backward; tiles of 128
+    bool few_f, few_b, few_dz, mid;  // few rows: forward, backward, dz alone; tiles of 128
     int parts;                       // bf16 parts of an operand of the products of tiles
     int Dp, strips, pieces;          // pieces: most that a plan may have
     int range, ranges, col_groups;   // few_ranges
@@ -552,6 +555,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.few_b = few_backward(c);
     L.parts = c.mode == REV_MODE_BF16 ? 1 : 3;
     const int es = L.parts == 1 ? 2 : 4;
+    L.few_dz = few_for_dz(c);
     L.Dp = (int)up(D, 128);
     L.Mp = up(M, 256);
     L.mid = mid_tiles_pay(M, V);
@@ -571,7 +575,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     if (!L.few_f || !L.few_b) L.w = L.Dp != D || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
     if (!L.few_b) {
         const int64_t all = L.Mp * up(V, 256);
-        L.lim.dz = std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
+        L.lim.dz = L.few_dz ? all : std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
         L.lim.tiles_d = (int)((D + 255) / 256);
         L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
@@ -644,7 +648,7 @@ struct VocabRunner {
         f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
         f.label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
         f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
-        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = M;
+        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = f.rows_out = M;
         f.range = L.range; f.ranges = L.ranges; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
         return f;
     }
@@ -674,11 +678,15 @@ struct VocabRunner {
     int backward_parts(T* dX, void* dparams) {
         VocabGemm g;
         RC(gemm_args(&g));
+        FewRows<T> f = few_args();
+        f.tile_dz = at<bf16>(L.dz);
+        f.rows_out = (int)up(M, 128);                              // dW goes over whole 128 rows
         for (int k = 0; k < L.pieces; ++k) {
             // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
             const int64_t tiles_v = ((V + k) / (k + 1) + 255) / 256;
             g.piece = k;
-            RC(vocab_logits<T>(s, g, true, dual(), L.mid, std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
+            if (L.few_dz) RC(few_logits<T>(s, f, true, false));
+            else RC(vocab_logits<T>(s, g, true, dual(), L.mid, std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
             if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
                               (int64_t)0, L.lim.dz);
             RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) : 0, dparams,
