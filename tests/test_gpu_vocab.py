@@ -21,6 +21,81 @@ def test_cross_entropy(shape, mode):
     VU.check(VU.make(M, D, V, mode, bias=M % 2 == 1, share=1.0 if M < 30 else 0.7, seed=M), "fp32")
 
 
+# sizes whose logits take tiles of 256: more than 128 of them
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape", [(300, 64, 16641), (513, 128, 11009), (769, 40, 8450)])
+def test_cross_entropy_in_large_tiles(shape, mode):
+    M, D, V = shape
+    print("[case] cross entropy", shape, mode, flush=True)
+    VU.check(VU.make(M, D, V, mode, bias=M % 2 == 1, share=0.8, seed=M), "fp32")
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("K,tau,labels", [(1, 1.0, False), (5, 1.0, True), (33, 2.0, False), (70, 4.0, True)])
+def test_distillation_in_large_tiles(K, tau, labels, mode):
+    print("[case] distillation", K, tau, labels, mode, flush=True)
+    c = VU.make(290, 64, 16700, mode, bias=labels, K=K, share=0.8, labels=labels, tau=tau, seed=K)
+    c["idx"][3] = 16699                        # one entry, K times, the vocabulary's last
+    c["idx"][40:140, 0] = np.arange(100) % 64  # many rows name the same 64 entries
+    if K > 1:
+        c["idx"][200] = np.arange(K)           # more than a tile's wavefront looks at in one go, with those around
+        c["idx"][192:224, 1:] = (np.arange(K - 1) * 7) % 61
+        if labels:
+            c["labels"][195] = c["idx"][195, 1]
+    VU.check(c, "fp32")
+
+
+@pytest.mark.parametrize("mode,M,D,V,K", [("bf16", 20000, 8, 16000, 3), ("fp32", 12000, 8, 10001, 3), ("bf16", 70001, 8, 5000, 0)])
+def test_several_pieces_of_the_vocabulary(mode, M, D, V, K):
+    """Sizes whose dz does not fit one piece, against torch in float64 on the GPU."""
+    print("[case] pieces", mode, M, D, V, K, flush=True)
+    c = VU.make(M, D, V, mode, K=K, tau=2.0, share=0.9, seed=21)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    f = VU.forward(cfg, c, a)
+    b = VU.backward(cfg, c, a, f["stats"])
+    W, bias = a["params"][:V * D].view(V, D).double(), a["params"][V * D:].double()
+    half, tol = VU.HALF[mode], 2e-5
+    dW, dWa, db, dba = torch.zeros_like(W), torch.zeros_like(W), torch.zeros_like(bias), torch.zeros_like(bias)
+    dX = torch.zeros(M, D, dtype=torch.float64, device="cuda")
+    for r in range(0, M, 4000):
+        s = slice(r, min(M, r + 4000))
+        x = a["X"][s].double()
+        z = x @ W.T + bias
+        y = a["labels"][s].long()
+        has = y >= 0
+        lse = torch.logsumexp(z, 1)
+        ce = torch.where(has, lse - z.gather(1, y.clamp(min=0)[:, None])[:, 0], torch.zeros_like(lse))
+        assert torch.linalg.norm(f["loss_ce"][s].double() - ce) <= tol * torch.linalg.norm(ce)
+        dz = torch.exp(z - lse[:, None])
+        dz[torch.arange(len(y), device="cuda"), y.clamp(min=0)] -= 1.0
+        dz *= (a["dce"][s].double() * has)[:, None]
+        if K:
+            idx = a["idx"][s].long()
+            on = idx >= 0
+            t = torch.where(on, a["logits"][s].double() / 2.0, torch.full_like(idx, -np.inf, dtype=torch.float64))
+            taught = on.any(1)
+            p = torch.where(on, torch.softmax(t, 1), torch.zeros_like(t))
+            logq = torch.log_softmax(z / 2.0, 1)
+            kd = 4.0 * torch.where(p > 0, p * (torch.log(p) - logq.gather(1, idx.clamp(min=0))), torch.zeros_like(p)).sum(1)
+            kd = torch.where(taught, kd, torch.zeros_like(kd))
+            assert torch.linalg.norm(f["loss_kd"][s].double() - kd) <= tol * torch.linalg.norm(kd)
+            g = logq.exp()
+            g.scatter_add_(1, idx.clamp(min=0), -p)
+            dz += g * (a["dkd"][s].double() * taught * 2.0)[:, None]
+        dX[s] = dz @ W
+        dW += dz.T @ x
+        dWa += dz.abs().T @ x.abs()
+        db += dz.sum(0)
+        dba += dz.abs().sum(0)
+    gW, gb = b["dparams"][:V * D].view(V, D).double(), b["dparams"][V * D:].double()
+    # dz rounded once, its float32 errors below 2e-5 of it, and sums of M terms in float32
+    lim = half * 1.01 + 2e-5 + M * VU.U
+    assert ((gW - dW).abs() <= lim * dWa + 1e-9).all() and ((gb - db).abs() <= lim * dba + 1e-9).all()
+    norm = 4 * half if mode == "bf16" else 2e-5
+    for got, want in ((gW, dW), (gb, db), (b["dX"].double(), dX)):
+        assert torch.linalg.norm(got - want) <= norm * torch.linalg.norm(want)
+
+
 @pytest.mark.parametrize("mode", ["bf16", "fp32"])
 @pytest.mark.parametrize("K,tau", [(1, 1.0), (3, 2.0), (64, 4.0), (65, 0.5), (256, 1.0)])
 @pytest.mark.parametrize("labels", [False, True])
