@@ -431,7 +431,16 @@ def rev_vocab_workspace_bytes(cfg: RevVocabCfg) -> int:
     return _check(lib().rev_vocab_workspace_bytes(ctypes.byref(cfg)))
 
 
-def _vocab_common(cfg, params, X, workspace, floats=(), ints=()):
+def _vocab_new(shape, dtype, X, stream):
+    """A tensor on the device of X for a call on `stream`: allocated for the current stream, so kept from being used again there before the
+    call's work is done if that is on another one."""
+    t = torch.empty(shape, dtype=dtype, device=X.device)
+    if stream is not None:
+        t.record_stream(stream)
+    return t
+
+
+def _vocab_common(cfg, params, X, workspace, stream, floats=(), ints=()):
     """Checks what the four calls have in common and returns the workspace.  floats, ints: (tensor or None, shape) of float32 and int32."""
     _want(params, param_dtype(cfg), (rev_vocab_param_count(cfg),))
     _want(X, param_dtype(cfg), (cfg.rows, cfg.d_model))
@@ -442,7 +451,7 @@ def _vocab_common(cfg, params, X, workspace, floats=(), ints=()):
                 assert t.device == X.device, "tensors of different devices"
     assert params.device == X.device, "tensors of different devices"
     if workspace is None:
-        return torch.empty(rev_vocab_workspace_bytes(cfg), dtype=torch.uint8, device=X.device)
+        return _vocab_new(rev_vocab_workspace_bytes(cfg), torch.uint8, X, stream)
     _want(workspace, torch.uint8)
     return workspace
 
@@ -457,29 +466,29 @@ def _vocab_call(name, X, stream, *args):
             _check(getattr(lib(), name)(*args, handle))
 
 
-def _vocab_out(out, name, shape, dtype, X):
+def _vocab_out(out, name, shape, dtype, X, stream):
     t = (out or {}).get(name)
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=X.device)
+        return _vocab_new(shape, dtype, X, stream)
     _want(t, dtype, shape)
     return t
 
 
-def _vocab_grads(cfg, X, out, want):
+def _vocab_grads(cfg, X, out, want, stream):
     assert want and set(want) <= {"dX", "dparams"}, "want: dX, dparams or both"
     res = {}
     if "dX" in want:
-        res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X)
+        res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X, stream)
     if "dparams" in want:
         dtype = torch.bfloat16 if cfg.grad_mode == REV_MODE_BF16 else torch.float32
-        res["dparams"] = _vocab_out(out, "dparams", (rev_vocab_param_count(cfg),), dtype, X)
+        res["dparams"] = _vocab_out(out, "dparams", (rev_vocab_param_count(cfg),), dtype, X, stream)
     return res
 
 
 def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=None):
     """Softmax cross entropy of the rows of X over the vocabulary: {"loss", "lse"}, float32 [rows]; labels int32 [rows]."""
-    ws = _vocab_common(cfg, params, X, workspace, ints=[(labels, (cfg.rows,))])
-    loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X) for n in ("loss", "lse"))
+    ws = _vocab_common(cfg, params, X, workspace, stream, ints=[(labels, (cfg.rows,))])
+    loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X, stream) for n in ("loss", "lse"))
     _vocab_call("rev_xent_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(ws),
                 ws.numel())
     return {"loss": loss, "lse": lse}
@@ -487,8 +496,8 @@ def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=No
 
 def rev_xent_backward(cfg, params, X, labels, lse, dloss, workspace=None, stream=None, out=None, want=("dX", "dparams")):
     """Gradients of sum(dloss * loss), with the lse of the forward call: the members of `want`."""
-    ws = _vocab_common(cfg, params, X, workspace, [(lse, (cfg.rows,)), (dloss, (cfg.rows,))], ints=[(labels, (cfg.rows,))])
-    res = _vocab_grads(cfg, X, out, want)
+    ws = _vocab_common(cfg, params, X, workspace, stream, [(lse, (cfg.rows,)), (dloss, (cfg.rows,))], ints=[(labels, (cfg.rows,))])
+    res = _vocab_grads(cfg, X, out, want, stream)
     _vocab_call("rev_xent_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(lse), _ptr(dloss),
                 _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws), ws.numel())
     return res
@@ -498,10 +507,11 @@ def rev_distill_forward(cfg, params, X, teacher_idx, teacher_logits, labels=None
     """Divergence from a teacher's top_k logits (int32 and float32 [rows, top_k]): {"loss", "lse"}, lse float32 [2, rows]; with labels
     their cross entropy as "loss_ce" too."""
     top = (cfg.rows, cfg.top_k)
-    ws = _vocab_common(cfg, params, X, workspace, [(teacher_logits, top)], ints=[(labels, (cfg.rows,)), (teacher_idx, top)])
-    res = {"loss": _vocab_out(out, "loss", (cfg.rows,), torch.float32, X), "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X)}
+    ws = _vocab_common(cfg, params, X, workspace, stream, [(teacher_logits, top)], ints=[(labels, (cfg.rows,)), (teacher_idx, top)])
+    res = {"loss": _vocab_out(out, "loss", (cfg.rows,), torch.float32, X, stream),
+           "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X, stream)}
     if labels is not None:
-        res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X)
+        res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X, stream)
     _vocab_call("rev_distill_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
                 _ptr(teacher_logits), _ptr(res.get("loss_ce")), _ptr(res["loss"]), _ptr(res["lse"]), _ptr(ws), ws.numel())
     return res
@@ -511,9 +521,9 @@ def rev_distill_backward(cfg, params, X, teacher_idx, teacher_logits, lse, dloss
                          out=None, want=("dX", "dparams")):
     """Gradients of sum(dloss * loss) (+ sum(dloss_ce * loss_ce) with labels), with the lse of the forward call."""
     top, row = (cfg.rows, cfg.top_k), (cfg.rows,)
-    ws = _vocab_common(cfg, params, X, workspace, [(teacher_logits, top), (lse, (2, cfg.rows)), (dloss, row), (dloss_ce, row)],
+    ws = _vocab_common(cfg, params, X, workspace, stream, [(teacher_logits, top), (lse, (2, cfg.rows)), (dloss, row), (dloss_ce, row)],
                        ints=[(labels, row), (teacher_idx, top)])
-    res = _vocab_grads(cfg, X, out, want)
+    res = _vocab_grads(cfg, X, out, want, stream)
     _vocab_call("rev_distill_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
                 _ptr(teacher_logits), _ptr(lse), _ptr(dloss_ce), _ptr(dloss), _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws),
                 ws.numel())

@@ -46,7 +46,8 @@ struct VocabGemm {
     bf16* dz;                       // a part [rows, width] of a piece
     float* acc;                     // dx, 65536 floats per tile and range
     int64_t Mp, dz_part;            // dz_part: elements from a part of dz to the next
-    int V, D, Dp, ldw, piece;       // piece: its number (backward)
+    int V, D, Dp, ldw;
+    int piece, span;                // piece: its number; span: its width in the forward pass, a multiple of 256
     int losses;                     // whose exponentials without `dual`: LOSS_CE, LOSS_KD or both (tau = 1)
     float inv_tau;
 };

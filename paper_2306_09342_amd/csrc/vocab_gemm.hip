@@ -333,7 +333,7 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     const TileLane t;
     const VocabPlan pl = *p.plan;
     const int tiles_m = __builtin_amdgcn_readfirstlane(pl.rows >> 8);
-    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.V, v0 = GRAD ? width * p.piece : 0, n = min(width, p.V - v0);
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span, v0 = width * p.piece, n = min(width, p.V - v0);
     const int tiles_n = n > 0 ? (n + 255) >> 8 : 0;
     TileRun run(tiles_m * tiles_n);
     if (run.done()) return;
@@ -492,7 +492,7 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const VocabPlan pl = *p.plan;
     const int rows_m = __builtin_amdgcn_readfirstlane((pl.count + 127) >> 7);
-    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.V, v0 = GRAD ? width * p.piece : 0, n = min(width, p.V - v0);
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span, v0 = width * p.piece, n = min(width, p.V - v0);
     const int tiles_n = n > 0 ? GRAD ? (n + 255) / 256 * 2 : (n + 127) >> 7 : 0, tiles = rows_m * tiles_n;    // dz is whole tiles of 256
     if ((int)blockIdx.x >= tiles) return;
     const int tile = xcd_remap(blockIdx.x, tiles), gn = tiles_n <= 8 ? tiles_n : 8, per_group = gn * rows_m, tg = tile / per_group;

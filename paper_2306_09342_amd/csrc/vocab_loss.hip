@@ -369,10 +369,12 @@ __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const floa
 
 // The same for 64 rows per workgroup.  stats: [strips][N][Mp] = maximum m of a strip, sums of exp(z - m) and exp((z - m) / tau), the
 // second with N = 3 only, the first in its place if only the teacher's loss is wanted.  A lane per row and 16 wavefronts over
-// the strips; then a wavefront per row over the teacher's entries.
+// the strips; then a wavefront per row over the teacher's entries.  Where the vocabulary comes in several pieces, `carry` is one more
+// strip, of the pieces before, and what a piece that is not the last leaves in the place of losses.
 template <int N>
 __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t Mp, const float* __restrict__ zs,
-                                                      const uint8_t* __restrict__ flags, RowResults out) {
+                                                      const uint8_t* __restrict__ flags, RowResults out, float* __restrict__ carry, bool first_piece,
+                                                      bool last_piece) {
     __shared__ float sh[3][16][64];
     __shared__ float row[3][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, count = v.plan->count;
@@ -381,6 +383,11 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
     const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
     float m = -INFINITY, s0 = 0.f, s1 = 0.f;
     const float* at = stats + i0 + lane;
+    if (w == 0 && !first_piece && i0 + lane < count) {
+        m = carry[i0 + lane];
+        s0 = carry[Mp + i0 + lane];
+        if (N == 3) s1 = carry[2 * Mp + i0 + lane];
+    }
     if (i0 + lane < count)
         for (int p0 = w; p0 < strips; p0 += 64) {
             float a[4][N];
@@ -410,7 +417,13 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
             if (N == 3) t1 += sh[2][k][lane] * expf(d * v.inv_tau);
         }
         row[0][lane] = top; row[1][lane] = logf(t0); row[2][lane] = logf(N == 3 ? t1 : t0);
+        if (!last_piece && i0 + lane < count) {
+            carry[i0 + lane] = top;
+            carry[Mp + i0 + lane] = top == -INFINITY ? 0.f : t0;
+            if (N == 3) carry[2 * Mp + i0 + lane] = top == -INFINITY ? 0.f : t1;
+        }
     }
+    if (!last_piece) return;
     __syncthreads();
     if (w == 0 && i0 + lane < count) {
         const int i = i0 + lane, r = v.list[i];
@@ -539,12 +552,15 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 // and 1024 MB: 8.31, 7.46, 7.34, 7.28 ms; 4096 x 768 to 50265 1.54, 1.50, 1.44, 1.45.  Fewer pieces have fuller rounds of tiles
 // and fewer passes over dx; that 256 MB would stay in the memory-side cache does not make up for them.
 constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
+// the statistics of a piece in the forward pass, three per 128 entries of a row, or those of 256 entries if that is more
+constexpr int64_t VOCAB_STATS_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, label_dz, zs, stats, xc, w, dz, acc, dzf, parts_dx, total;
+    int64_t plan, flags, place, list, coef, label_dz, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, total;
     int64_t Mp, ldz;                 // ldz: of dz in float32
     bool few_f, few_b, few_dz, mid;  // few rows: forward, backward, dz alone; tiles of 128
     int parts;                       // bf16 parts of an operand of the products of tiles
-    int Dp, strips, pieces;          // pieces: most that a plan may have
+    int Dp, strips, pieces;          // strips of a piece forward; pieces: most that a plan may have backward
+    int span;                        // width of a piece forward (tiles of 256)
     int range, ranges, col_groups;   // few_ranges
     PlanLimits lim;
 };
@@ -559,7 +575,9 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.Dp = (int)up(D, 128);
     L.Mp = up(M, 256);
     L.mid = mid_tiles_pay(M, V);
-    L.strips = (int)(L.few_f ? (V + 63) / 64 : L.mid ? (V + 127) / 128 * 2 : (V + 255) / 256 * 2);
+    const bool large = !L.few_f && !L.mid;
+    L.span = (int)(large ? std::min(std::max(VOCAB_STATS_BYTES * 128 / 12 / L.Mp / 256 * 256, (int64_t)256), up(V, 256)) : up(V, 256));
+    L.strips = (int)(L.few_f ? (V + 63) / 64 : L.mid ? (V + 127) / 128 * 2 : L.span / 128);
     int64_t at = 0;
     auto take = [&](int64_t bytes) { const int64_t o = at; at += up(bytes, 256); return o; };
     L.plan = take(sizeof(VocabPlan));
@@ -570,6 +588,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.label_dz = take(8 * L.Mp);
     L.zs = take(4 * M * (c.top_k + 1));
     L.stats = take(12 * (L.few_f ? M : L.Mp) * L.strips);
+    if (large) L.carry = take(12 * L.Mp);
     // the rows' copy: their own type, or parts of it, in the place of the larger
     L.xc = take(L.Mp * L.Dp * (L.parts == 1 ? 2 : 6));
     if (!L.few_f || !L.few_b) L.w = L.Dp != D || L.parts > 1 ? take(2 * L.parts * V * L.Dp) : 0;
@@ -634,13 +653,17 @@ struct VocabRunner {
         LAUNCH((gather_kernel<T, P>), rows, block, v, g, flags());
         return REV_OK;
     }
-    int join(const RowResults& out) {
+    int join(const RowResults& out, int piece = 0, int pieces = 1) {
         ProfScope ps(K_REDUCE, s, 12.0 * M * L.strips);
         const int64_t kind = L.strips;
-        if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
-        else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), L.strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
-        else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
-        else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), L.strips, L.Mp, at<float>(L.zs), flags(), out);
+        const int strips = L.few_f || L.mid ? L.strips : (int)((std::min<int64_t>(L.span, V - (int64_t)piece * L.span) + 255) / 256 * 2);
+        float* carry = at<float>(L.carry);
+        if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry,
+                                piece == 0, piece + 1 == pieces);
+        else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry, piece == 0,
+                    piece + 1 == pieces);
         return REV_OK;
     }
     FewRows<T> few_args() {
@@ -672,8 +695,14 @@ struct VocabRunner {
     int forward_parts(const RowResults& out) {
         VocabGemm g;
         RC(gemm_args(&g));
-        RC(vocab_logits<T>(s, g, false, dual(), L.mid, L.Mp / 256 * ((V + 255) / 256)));
-        return join(out);
+        const int pieces = (V + L.span - 1) / L.span;
+        g.span = L.span;
+        for (int k = 0; k < pieces; ++k) {
+            g.piece = k;
+            RC(vocab_logits<T>(s, g, false, dual(), L.mid, L.Mp / 256 * (L.span / 256)));
+            RC(join(out, k, pieces));
+        }
+        return REV_OK;
     }
     int backward_parts(T* dX, void* dparams) {
         VocabGemm g;
