@@ -190,24 +190,43 @@ __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<
         if (flags & HAS_TEACHER) { c.z = g.cot.dkd[r] / v.inv_tau; c.w = g.cot.lse_tau[r]; }
         if (threadIdx.x == 0) g.coef[i] = c;
     }
+    // four entries of a wavefront at a time, so that four rows of W are under way
     const int lane = threadIdx.x & 63;
-    for (int e = threadIdx.x >> 6; e <= v.K; e += 4) {
-        const int n = entry_of(v, r, e);
-        float s = 0.f;
-        if (n >= 0) {
-            const T* w = g.params + (int64_t)n * g.D;
-            for (int d = lane * E; d < g.D; d += 64 * E) {
+    for (int e0 = (threadIdx.x >> 6) * 4; e0 <= v.K; e0 += 16) {
+        int n[4];
+        const T* w[4];
+        float sum[4] = {};
 #pragma unroll
-                for (int q = 0; q < E; q += 4) {
-                    const f4 a = load4(x + d + q), b = load4(w + d + q);
-                    s = fmaf(a.x, b.x, s); s = fmaf(a.y, b.y, s); s = fmaf(a.z, b.z, s); s = fmaf(a.w, b.w, s);
+        for (int u = 0; u < 4; ++u) {
+            n[u] = e0 + u <= v.K ? entry_of(v, r, e0 + u) : -1;
+            w[u] = g.params + (int64_t)max(n[u], 0) * g.D;
+        }
+        for (int d = lane * E; d < g.D; d += 64 * E) {
+            f4 a[E / 4];
+#pragma unroll
+            for (int q = 0; q < E / 4; ++q) a[q] = load4(x + d + 4 * q);
+            uint4 b[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) b[u] = n[u] >= 0 ? *reinterpret_cast<const uint4*>(w[u] + d) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const T* f = reinterpret_cast<const T*>(&b[u]);
+#pragma unroll
+                for (int q = 0; q < E / 4; ++q) {
+                    const f4 c = load4(f + 4 * q);
+                    sum[u] = fmaf(a[q].x, c.x, sum[u]); sum[u] = fmaf(a[q].y, c.y, sum[u]);
+                    sum[u] = fmaf(a[q].z, c.z, sum[u]); sum[u] = fmaf(a[q].w, c.w, sum[u]);
                 }
             }
         }
-        s = wave_sum(s);
-        if (n >= 0 && v.bias) s += to_f(g.params[(int64_t)v.V * g.D + n]);
-        if (lane == 0) g.zs[(int64_t)i * (v.K + 1) + e] = s;
-        if (e == 0 && lane == 0 && g.label_dz) g.label_dz[i] = {n, dense_dz(c, s, v.inv_tau) - c.x};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (e0 + u > v.K) break;
+            float z = wave_sum(sum[u]);
+            if (n[u] >= 0 && v.bias) z += to_f(g.params[(int64_t)v.V * g.D + n[u]]);
+            if (lane == 0) g.zs[(int64_t)i * (v.K + 1) + e0 + u] = z;
+            if (e0 + u == 0 && lane == 0 && g.label_dz) g.label_dz[i] = {n[u], dense_dz(c, z, v.inv_tau) - c.x};
+        }
     }
 }
 
