@@ -192,8 +192,21 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
     const int count = __builtin_amdgcn_readfirstlane(p.plan->count);
     const int r = blockIdx.x / p.col_groups, cg = blockIdx.x - r * p.col_groups, P = p.range + 1;
     const int v0 = r * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
-    for (int i = wave; i < rows32; i += 4)
-        for (int c = lane; c < p.range; c += 64) dzs[i * P + c] = i < count && c < nv ? p.dz[i * p.ldz + v0 + c] : 0.f;
+    // chunks of 32 entries of a row, two per wavefront, eight of each in flight
+    const int per = p.range >> 5, chunks = rows32 * per;
+    for (int k0 = wave * 2 + g; k0 < chunks; k0 += 64) {
+        float u[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int k = k0 + 8 * q, i = k / per, c = (k - i * per) * 32 + fr;
+            u[q] = i < count && c < nv ? p.dz[i * p.ldz + v0 + c] : 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int k = k0 + 8 * q, i = k / per, c = (k - i * per) * 32 + fr;
+            if (k < chunks) dzs[i * P + c] = u[q];
+        }
+    }
     __syncthreads();
     if (db && dparams && cg == 0)
         for (int c = threadIdx.x; c < nv; c += 256) {

@@ -332,6 +332,21 @@ __device__ __forceinline__ void teacher_loss(const VocabRows& v, int r, const fl
     *lse_tau = top * v.inv_tau + log_s;
 }
 
+// What a row's statistics come to, by a wavefront.
+__device__ __forceinline__ void row_losses(const VocabRows& v, int i, float top, float log0, float log1, const float* zs, const uint8_t* flags, int lane,
+                                           float* loss_ce, float* lse, float* loss_kd, float* lse_tau) {
+    const int r = v.list[i];
+    const float* z = zs + (int64_t)i * (v.K + 1);
+    const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
+    float kd = 0.f, l1 = 0.f;
+    if (loss_kd && (flags[r] & HAS_TEACHER)) teacher_loss(v, r, z, top, log1, lane, &kd, &l1);
+    if (lane == 0) {
+        if (loss_ce) loss_ce[r] = has ? log0 + (top - z[0]) : 0.f;
+        lse[r] = has ? top + log0 : 0.f;
+        if (loss_kd) { loss_kd[r] = kd; lse_tau[r] = l1; }
+    }
+}
+
 // The statistics of a row joined, and its losses, a workgroup per row: for few rows.  stats: see FewRows and losses_kernel.
 template <int N>
 __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t stat_row, int64_t stat_kind,
@@ -373,47 +388,38 @@ __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const floa
         t0 += sh[1][k] * expf((sh[0][k] - top) * rate0);
         if (N == 3) t1 += sh[2][k] * expf((sh[0][k] - top) * v.inv_tau);
     }
-    const float log0 = logf(t0), log1 = N == 3 ? logf(t1) : log0;
-    const int r = v.list[i];
-    const float* z = zs + (int64_t)i * (v.K + 1);
-    const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
-    float kd = 0.f, l1 = 0.f;
-    if (loss_kd && (flags[r] & HAS_TEACHER)) teacher_loss(v, r, z, top, log1, lane, &kd, &l1);
-    if (lane == 0) {
-        if (loss_ce) loss_ce[r] = has ? log0 + (top - z[0]) : 0.f;
-        lse[r] = has ? top + log0 : 0.f;
-        if (loss_kd) { loss_kd[r] = kd; lse_tau[r] = l1; }
-    }
+    row_losses(v, i, top, logf(t0), logf(N == 3 ? t1 : t0), zs, flags, lane, loss_ce, lse, loss_kd, lse_tau);
 }
 
-// The same for 64 rows per workgroup.  stats: [strips][N][Mp] = maximum m of a strip, sums of exp(z - m) and exp((z - m) / tau), the
-// second with N = 3 only, the first in its place if only the teacher's loss is wanted.  A lane per row and 16 wavefronts over
-// the strips; then a wavefront per row over the teacher's entries.  Where the vocabulary comes in several pieces, `carry` is one more
-// strip, of the pieces before, and what a piece that is not the last leaves in the place of losses.
+// The same for 16 rows per workgroup.  stats: [strips][N][Mp] = maximum m of a strip, sums of exp(z - m) and exp((z - m) / tau), the
+// second with N = 3 only, the first in its place if only the teacher's loss is wanted.  64 threads per row over the strips, then a
+// wavefront per row.  Where the vocabulary comes in several pieces, `carry` is one more strip, of the pieces before, and what a piece
+// that is not the last leaves in the place of losses.
+constexpr int JOIN_ROWS = 16;
 template <int N>
 __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t Mp, const float* __restrict__ zs,
                                                       const uint8_t* __restrict__ flags, RowResults out, float* __restrict__ carry, bool first_piece,
                                                       bool last_piece) {
-    __shared__ float sh[3][16][64];
-    __shared__ float row[3][64];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, i0 = blockIdx.x * 64, count = v.plan->count;
+    __shared__ float sh[3][JOIN_ROWS][65];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = threadIdx.x & (JOIN_ROWS - 1), part = threadIdx.x / JOIN_ROWS;
+    const int i0 = blockIdx.x * JOIN_ROWS, count = v.plan->count;
     float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
     if (i0 >= count) return;
     const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
     float m = -INFINITY, s0 = 0.f, s1 = 0.f;
-    const float* at = stats + i0 + lane;
-    if (w == 0 && !first_piece && i0 + lane < count) {
-        m = carry[i0 + lane];
-        s0 = carry[Mp + i0 + lane];
-        if (N == 3) s1 = carry[2 * Mp + i0 + lane];
-    }
-    if (i0 + lane < count)
-        for (int p0 = w; p0 < strips; p0 += 64) {
+    if (i0 + row < count) {
+        const float* at = stats + i0 + row;
+        if (part == 0 && !first_piece) {
+            m = carry[i0 + row];
+            s0 = carry[Mp + i0 + row];
+            if (N == 3) s1 = carry[2 * Mp + i0 + row];
+        }
+        for (int p0 = part; p0 < strips; p0 += 256) {
             float a[4][N];
 #pragma unroll
             for (int u = 0; u < 4; ++u)
 #pragma unroll
-                for (int k = 0; k < N; ++k) a[u][k] = p0 + 16 * u < strips ? at[((int64_t)(p0 + 16 * u) * N + k) * Mp] : k ? 0.f : -INFINITY;
+                for (int k = 0; k < N; ++k) a[u][k] = p0 + 64 * u < strips ? at[((int64_t)(p0 + 64 * u) * N + k) * Mp] : k ? 0.f : -INFINITY;
             const float top = fmaxf(fmaxf(fmaxf(a[0][0], a[1][0]), fmaxf(a[2][0], a[3][0])), m);
             if (top == -INFINITY) continue;
             s0 *= expf((m - top) * rate0);
@@ -425,38 +431,24 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
             }
             m = top;
         }
-    sh[0][w][lane] = m; sh[1][w][lane] = s0; sh[2][w][lane] = s1;
+    }
+    sh[0][row][part] = m; sh[1][row][part] = s0; sh[2][row][part] = s1;
     __syncthreads();
-    if (w == 0) {
-        float top = -INFINITY, t0 = 0.f, t1 = 0.f;
-        for (int k = 0; k < 16; ++k) top = fmaxf(top, sh[0][k][lane]);
-        for (int k = 0; k < 16; ++k) {
-            const float d = sh[0][k][lane] - top;
-            t0 += sh[1][k][lane] * expf(d * rate0);
-            if (N == 3) t1 += sh[2][k][lane] * expf(d * v.inv_tau);
+    const int i = i0 + w;
+    if (i >= count) return;
+    m = sh[0][w][lane];
+    const float top = wave_max(m), d = top == -INFINITY ? 0.f : m - top;
+    s0 = wave_sum(sh[1][w][lane] * expf(d * rate0));
+    if (N == 3) s1 = wave_sum(sh[2][w][lane] * expf(d * v.inv_tau));
+    if (!last_piece) {
+        if (lane == 0) {
+            carry[i] = top;
+            carry[Mp + i] = s0;
+            if (N == 3) carry[2 * Mp + i] = s1;
         }
-        row[0][lane] = top; row[1][lane] = logf(t0); row[2][lane] = logf(N == 3 ? t1 : t0);
-        if (!last_piece && i0 + lane < count) {
-            carry[i0 + lane] = top;
-            carry[Mp + i0 + lane] = top == -INFINITY ? 0.f : t0;
-            if (N == 3) carry[2 * Mp + i0 + lane] = top == -INFINITY ? 0.f : t1;
-        }
+        return;
     }
-    if (!last_piece) return;
-    __syncthreads();
-    if (w == 0 && i0 + lane < count) {
-        const int i = i0 + lane, r = v.list[i];
-        const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
-        if (loss_ce) loss_ce[r] = has ? row[1][lane] + (row[0][lane] - zs[(int64_t)i * (v.K + 1)]) : 0.f;
-        lse[r] = has ? row[0][lane] + row[1][lane] : 0.f;
-    }
-    if (!loss_kd) return;
-    for (int k = w; k < 64 && i0 + k < count; k += 16) {
-        const int i = i0 + k, r = v.list[i];
-        float kd = 0.f, l = 0.f;
-        if (flags[r] & HAS_TEACHER) teacher_loss(v, r, zs + (int64_t)i * (v.K + 1), row[0][k], row[2][k], lane, &kd, &l);
-        if (lane == 0) { loss_kd[r] = kd; lse_tau[r] = l; }
-    }
+    row_losses(v, i, top, logf(s0), logf(N == 3 ? s1 : s0), zs, flags, lane, loss_ce, lse, loss_kd, lse_tau);
 }
 
 // ---------------------------------------------------------------------------------
@@ -551,13 +543,13 @@ static int64_t few_blocks(int64_t M, int64_t V) { return (M + 63) / 64 * ((V + 6
 static bool few_forward(const rev_vocab_cfg& c) {
     return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 400;
 }
-// Backward.  bf16: V = 50265, 1 row: 87 / 78, 16: 81 / 98; V = 131072, D = 256, 4 rows: 96 / 70; V = 10007, 16 rows: 41 / 35, 64: 43 / 56; V = 1000, 8: 32
-// / 22, 64: 33 / 34.  float32, whose tiles need W in parts first: V = 50265, 1 row: 359 / 118, 64: 376 / 261; V = 10007, 128: 151 / 123; V =
-// 1000, 256: 106 / 72, 512: 127 / 122; V = 2000, D = 1024, 300: 136 / 115.
+// Backward.  bf16: V = 50265, 1 row: 87 / 76, 8: 87 / 81, 32: 81 / 106; V = 131072, D = 256, 4 rows: 97 / 70; V = 10007, 16 rows: 42 / 39, 32: 42 / 46;
+// V = 1000, 8: 26 / 22, 64: 27 / 30.  float32, whose tiles need W in parts first: V = 50265, 1 row: 359 / 118, 64: 378 / 259, 128: 395 / 491; V =
+// 10007, 128: 151 / 137; V = 1000, 512 (128 blocks): 127 / 87; V = 5003, D = 200, 333 (474): 101 / 91; D = 768, 256 (316): 132 / 140; D = 256, 500 (632):
+// 101 / 123; V = 20000, D = 384, 200 (1252): 175 / 192.
 static bool few_backward(const rev_vocab_cfg& c) {
-    const int64_t blocks = few_blocks(c.rows, c.vocab);
-    if (c.mode == REV_MODE_BF16) return c.rows <= 4 || (c.rows <= 32 && blocks <= 160);
-    return c.rows <= 64 || (c.rows <= 128 && c.vocab <= 16384) || (c.rows <= 512 && blocks <= 160);
+    if (c.mode == REV_MODE_BF16) return c.rows <= 8 || (c.rows <= 16 && c.vocab <= 16384);
+    return c.rows <= 64 || (c.rows <= 128 && c.vocab <= 16384) || (c.rows <= 512 && few_blocks(c.rows, c.vocab) <= 480);
 }
 // dz alone by them, the gradients in tiles (bf16).  V = 1000, 128 rows: 35 / 29, 512: 45 / 39; V = 10007, 128 rows: 54 / 53.
 static bool few_for_dz(const rev_vocab_cfg& c) { return c.mode == REV_MODE_BF16 && !few_backward(c) && few_blocks(c.rows, c.vocab) <= 160; }
@@ -679,9 +671,9 @@ struct VocabRunner {
         float* carry = at<float>(L.carry);
         if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
         else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
-        else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry,
+        else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, JOIN_ROWS), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry,
                                 piece == 0, piece + 1 == pieces);
-        else LAUNCH(losses_kernel<2>, blocks_of(M, 64), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry, piece == 0,
+        else LAUNCH(losses_kernel<2>, blocks_of(M, JOIN_ROWS), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry, piece == 0,
                     piece + 1 == pieces);
         return REV_OK;
     }
