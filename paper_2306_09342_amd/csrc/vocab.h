@@ -30,6 +30,14 @@ __device__ __forceinline__ float dense_dz(const float4& c, float z, float inv_ta
     return d;
 }
 
+// The first entry of piece k of a vocabulary and how many it has.  A launch may be for a piece that the plan does not come to, up to 2^12
+// pieces of 2^20 entries behind its end: n is 0 there, and v0 nothing.
+struct Piece { int v0, n; };
+__device__ __forceinline__ Piece piece_of(int k, int width, int V) {
+    const int64_t v0 = (int64_t)k * width;
+    return {(int)v0, v0 < V ? min(width, V - (int)v0) : 0};
+}
+
 struct LabelDz { int label; float dz; };         // a row's label, and dz there
 
 constexpr int LOSS_CE = 1, LOSS_KD = 2;

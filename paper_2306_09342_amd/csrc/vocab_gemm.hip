@@ -333,8 +333,10 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     const TileLane t;
     const VocabPlan pl = *p.plan;
     const int tiles_m = __builtin_amdgcn_readfirstlane(pl.rows >> 8);
-    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span, v0 = width * p.piece, n = min(width, p.V - v0);
-    const int tiles_n = n > 0 ? (n + 255) >> 8 : 0;
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span;
+    const Piece piece = piece_of(p.piece, width, p.V);
+    const int v0 = piece.v0, n = piece.n;
+    const int tiles_n = (n + 255) >> 8;
     TileRun run(tiles_m * tiles_n);
     if (run.done()) return;
     const int gn = tiles_n <= 6 ? tiles_n : 4, per_group = gn * tiles_m;
@@ -492,8 +494,10 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave & 1, wn = wave >> 1;
     const VocabPlan pl = *p.plan;
     const int rows_m = __builtin_amdgcn_readfirstlane((pl.count + 127) >> 7);
-    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span, v0 = width * p.piece, n = min(width, p.V - v0);
-    const int tiles_n = n > 0 ? GRAD ? (n + 255) / 256 * 2 : (n + 127) >> 7 : 0, tiles = rows_m * tiles_n;    // dz is whole tiles of 256
+    const int width = GRAD ? __builtin_amdgcn_readfirstlane(pl.width) : p.span;
+    const Piece piece = piece_of(p.piece, width, p.V);
+    const int v0 = piece.v0, n = piece.n;
+    const int tiles_n = GRAD ? (n + 255) / 256 * 2 : (n + 127) >> 7, tiles = rows_m * tiles_n;    // dz is whole tiles of 256
     if ((int)blockIdx.x >= tiles) return;
     const int tile = xcd_remap(blockIdx.x, tiles), gn = tiles_n <= 8 ? tiles_n : 8, per_group = gn * rows_m, tg = tile / per_group;
     const int in_grp = tile - tg * per_group, gw = min(gn, tiles_n - tg * gn);
@@ -610,8 +614,10 @@ __device__ __forceinline__ void dx_block(const VocabGemm& p, unsigned char* smem
     const TileLane t;
     const VocabPlan pl = *p.plan;
     const int tiles_d = (p.D + 255) >> 8, tiles = __builtin_amdgcn_readfirstlane((pl.rows >> 8) * tiles_d);
-    const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
-    if (n <= 0 || block >= tiles * pl.splits) return;
+    const int width = __builtin_amdgcn_readfirstlane(pl.width);
+    const Piece piece = piece_of(p.piece, width, p.V);
+    const int v0 = piece.v0, n = piece.n;
+    if (n == 0 || block >= tiles * pl.splits) return;
     const int lin = xcd_remap(block, tiles * pl.splits);
     const int split = __builtin_amdgcn_readfirstlane(lin / tiles), tile = __builtin_amdgcn_readfirstlane(lin - split * tiles);
     const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
@@ -737,8 +743,10 @@ template <typename TG, int P>
 __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem, TG* dparams, int db, int block) {
     const TileLane t;
     const VocabPlan pl = *p.plan;
-    const int width = __builtin_amdgcn_readfirstlane(pl.width), v0 = width * p.piece, n = min(width, p.V - v0);
-    if (n <= 0) return;
+    const int width = __builtin_amdgcn_readfirstlane(pl.width);
+    const Piece piece = piece_of(p.piece, width, p.V);
+    const int v0 = piece.v0, n = piece.n;
+    if (n == 0) return;
     const int tiles_v = (n + 255) >> 8, tiles_d = (p.D + 255) >> 8, tiles = tiles_v * tiles_d;
     const int64_t ldz = width;
     if (block >= tiles) {

@@ -465,9 +465,10 @@ __global__ __launch_bounds__(256) void sparse_dz_kernel(VocabRows v, const float
     const bool live = i < v.plan->count;
     if (n == 0) {
         ld = v.plan->width;
-        v0 *= (int)ld;
-        n = min((int)ld, v.V - v0);
-        if (n <= 0) return;
+        const Piece of = piece_of(v0, (int)ld, v.V);
+        v0 = of.v0;
+        n = of.n;
+        if (n == 0) return;
     }
     int mine[5];
     if (live) {

@@ -267,6 +267,37 @@ def test_many_rows_of_few_columns(mode):
     assert torch.linalg.norm(b["dX"].double() - dX) <= (4 * half if mode == "bf16" else 2e-5) * torch.linalg.norm(dX)
 
 
+def test_many_pieces_that_no_row_needs():
+    """So many rows, of which so few count, that the pieces which all of them would need lie as far as 2^32 entries behind the vocabulary."""
+    M, D, V, on = 524800, 8, 1 << 20, 200
+    g = torch.Generator(device="cuda").manual_seed(22)
+    guarded = torch.full((V * D + 2 * 4096,), 7.0, device="cuda")
+    params = torch.randn(V * D, generator=g, device="cuda").bfloat16()
+    X = torch.randn(M, D, generator=g, device="cuda").bfloat16()
+    rows = torch.arange(on, device="cuda") * 2600
+    labels = torch.full((M,), -100, dtype=torch.int32, device="cuda")
+    labels[rows] = torch.randint(0, V, (on,), generator=g, device="cuda", dtype=torch.int32)
+    dloss = torch.rand(M, generator=g, device="cuda")
+    cfg = B.make_vocab_cfg(M, D, V, "bf16", bias=False)
+    f = B.rev_xent_forward(cfg, params, X, labels)
+    b = B.rev_xent_backward(cfg, params, X, labels, f["lse"], dloss, out={"dparams": guarded[4096:-4096]})
+    W, x, y = params.view(V, D).double(), X[rows].double(), labels[rows].long()
+    z = x @ W.T
+    lse = torch.logsumexp(z, 1)
+    ce = lse - z.gather(1, y[:, None])[:, 0]
+    assert torch.linalg.norm(f["loss"][rows].double() - ce) <= 2e-5 * torch.linalg.norm(ce)
+    dz = torch.exp(z - lse[:, None])
+    dz[torch.arange(on, device="cuda"), y] -= 1.0
+    dz *= dloss[rows].double()[:, None]
+    half = VU.HALF["bf16"]
+    for got, want in ((b["dparams"].view(V, D), dz.T @ x), (b["dX"][rows], dz @ W)):
+        assert torch.linalg.norm(got.double() - want) <= 4 * half * torch.linalg.norm(want)
+    assert (guarded[:4096] == 7.0).all() and (guarded[-4096:] == 7.0).all()
+    off = torch.ones(M, dtype=torch.bool, device="cuda")
+    off[rows] = False
+    assert not f["loss"][off].any() and not b["dX"][off].any()
+
+
 @pytest.mark.parametrize("mode", ["bf16", "fp32"])
 def test_repeats_bit_for_bit_on_any_stream_and_two_at_once(mode):
     c = VU.make(600, 256, 3001, mode, K=4, share=0.7, tau=2.0, seed=13)
