@@ -293,7 +293,8 @@ __global__ __launch_bounds__(256) void select_gather_kernel(VocabRows v, GatherA
     gather_row<T, P>(v, g, i, live, live ? found[0] : 0, live ? found[1] : 0);
 }
 
-// The teacher's probabilities of a row, entry e = 1 + lane + 64 q in p[q] (0: none), and log p_k = t_k / tau - log_norm.
+// The teacher's probabilities of a row, entry e = 1 + lane + 64 q in p[q] (0: none), and log p_k = t_k - log_norm, t_k = (its logit - the
+// largest) / tau: the difference first, since a lowest value has no room for a factor or a logarithm.
 struct Teacher { float p[4], t[4], log_norm; };
 __device__ __forceinline__ Teacher teacher_of(const VocabRows& v, int r, int lane) {
     Teacher a;
@@ -301,18 +302,19 @@ __device__ __forceinline__ Teacher teacher_of(const VocabRows& v, int r, int lan
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int k = lane + 64 * q;
-        a.t[q] = k < v.K && entry_of(v, r, k + 1) >= 0 ? v.logits[(int64_t)r * v.K + k] * v.inv_tau : -INFINITY;
+        a.t[q] = k < v.K && entry_of(v, r, k + 1) >= 0 ? v.logits[(int64_t)r * v.K + k] : -INFINITY;
         m = fmaxf(m, a.t[q]);
     }
     m = wave_max(m);
     float s = 0.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        a.p[q] = a.t[q] == -INFINITY ? 0.f : expf(a.t[q] - m);
+        if (a.t[q] != -INFINITY) a.t[q] = (a.t[q] - m) * v.inv_tau;
+        a.p[q] = expf(a.t[q]);
         s += a.p[q];
     }
     s = wave_sum(s);
-    a.log_norm = m + logf(s);
+    a.log_norm = logf(s);
 #pragma unroll
     for (int q = 0; q < 4; ++q) a.p[q] = a.p[q] / s;
     return a;

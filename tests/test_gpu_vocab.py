@@ -192,6 +192,19 @@ def test_teachers_with_repeats_and_gaps(mode):
     VU.check(c)
 
 
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("tau", [0.25, 1.0, 3.0])
+def test_teachers_that_know_lowest_values_alone(tau, mode):
+    """They are equally likely, as entries of logit 0 are: the same results, bit for bit."""
+    c = VU.make(30, 64, 200, mode, K=70, tau=tau, seed=19)
+    c["logits"][::2] = 0.0
+    ref, _ = VU.check(c)
+    c["logits"][::2] = np.finfo(np.float32).min
+    got = VU.run(c)
+    for k in ref:
+        assert torch.equal(ref[k], got[k]), k
+
+
 def test_a_student_that_is_its_teacher():
     """The gradient is a difference of two nearly equal probabilities: taken in float32, rounded once."""
     c = VU.make(20, 64, 120, "bf16", bias=False, K=120, tau=2.0, labels=False, seed=9)
