@@ -367,13 +367,13 @@ __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const floa
 #pragma unroll
             for (int k = 0; k < N; ++k) a[u][k] = p0 + 256 * u < strips ? at[k * stat_kind + p0 + 256 * u] : k ? 0.f : -INFINITY;
         const float top = fmaxf(fmaxf(fmaxf(a[0][0], a[1][0]), fmaxf(a[2][0], a[3][0])), m);
-        if (top == -INFINITY) continue;
-        s0 *= expf((m - top) * rate0);
-        if (N == 3) s1 *= expf((m - top) * v.inv_tau);
+        const float ref = top == -INFINITY ? 0.f : top;        // (sums are 0 or NaN there)
+        s0 *= expf((m - ref) * rate0);
+        if (N == 3) s1 *= expf((m - ref) * v.inv_tau);
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            s0 += a[u][1] * expf((a[u][0] - top) * rate0);
-            if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - top) * v.inv_tau);
+            s0 += a[u][1] * expf((a[u][0] - ref) * rate0);
+            if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - ref) * v.inv_tau);
         }
         m = top;
     }
@@ -383,12 +383,12 @@ __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const floa
     if (lane == 0) { sh[0][w] = wm; sh[1][w] = s0; sh[2][w] = s1; }
     __syncthreads();
     if (w) return;
-    const float top = fmaxf(fmaxf(sh[0][0], sh[0][1]), fmaxf(sh[0][2], sh[0][3]));
+    const float top = fmaxf(fmaxf(sh[0][0], sh[0][1]), fmaxf(sh[0][2], sh[0][3])), ref = top == -INFINITY ? 0.f : top;
     float t0 = 0.f, t1 = 0.f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        t0 += sh[1][k] * expf((sh[0][k] - top) * rate0);
-        if (N == 3) t1 += sh[2][k] * expf((sh[0][k] - top) * v.inv_tau);
+        t0 += sh[1][k] * expf((sh[0][k] - ref) * rate0);
+        if (N == 3) t1 += sh[2][k] * expf((sh[0][k] - ref) * v.inv_tau);
     }
     row_losses(v, i, top, logf(t0), logf(N == 3 ? t1 : t0), zs, flags, lane, loss_ce, lse, loss_kd, lse_tau);
 }
@@ -423,13 +423,13 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
 #pragma unroll
                 for (int k = 0; k < N; ++k) a[u][k] = p0 + 64 * u < strips ? at[((int64_t)(p0 + 64 * u) * N + k) * Mp] : k ? 0.f : -INFINITY;
             const float top = fmaxf(fmaxf(fmaxf(a[0][0], a[1][0]), fmaxf(a[2][0], a[3][0])), m);
-            if (top == -INFINITY) continue;
-            s0 *= expf((m - top) * rate0);
-            if (N == 3) s1 *= expf((m - top) * v.inv_tau);
+            const float ref = top == -INFINITY ? 0.f : top;        // (sums are 0 or NaN there)
+            s0 *= expf((m - ref) * rate0);
+            if (N == 3) s1 *= expf((m - ref) * v.inv_tau);
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                s0 += a[u][1] * expf((a[u][0] - top) * rate0);
-                if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - top) * v.inv_tau);
+                s0 += a[u][1] * expf((a[u][0] - ref) * rate0);
+                if (N == 3) s1 += a[u][N - 1] * expf((a[u][0] - ref) * v.inv_tau);
             }
             m = top;
         }

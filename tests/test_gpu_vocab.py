@@ -162,6 +162,22 @@ def test_entries_taken_out_by_the_bias(low, mode):
     VU.check(c)
 
 
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,V", [(6, 900), (300, 1100), (300, 17000)])
+def test_a_row_that_is_not_a_number_keeps_it_to_itself(M, V, mode):
+    c = VU.make(M, 64, V, mode, K=3, tau=2.0, seed=20)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    one = VU.forward(cfg, c, a)
+    one.update(VU.backward(cfg, c, a, one["stats"], want=("dX",)))
+    a["X"][2, 5] = float("nan")
+    two = VU.forward(cfg, c, a)
+    two.update(VU.backward(cfg, c, a, two["stats"], want=("dX",)))
+    for k in ("loss_ce", "loss_kd", "lse", "lse_tau", "dX"):
+        assert torch.isnan(two[k][2]).all(), k
+        two[k][2] = one[k][2]
+        assert torch.equal(one[k], two[k]), k
+
+
 def test_a_label_that_the_bias_took_out():
     c = VU.make(4, 64, 50, "fp32", seed=6)
     c["params"][50 * 64 + 7] = -np.inf
