@@ -453,6 +453,7 @@ def _vocab_common(cfg, params, X, workspace, stream, floats=(), ints=()):
     if workspace is None:
         return _vocab_new(rev_vocab_workspace_bytes(cfg), torch.uint8, X, stream)
     _want(workspace, torch.uint8)
+    assert workspace.device == X.device, "tensors of different devices"
     return workspace
 
 
@@ -471,6 +472,7 @@ def _vocab_out(out, name, shape, dtype, X, stream):
     if t is None:
         return _vocab_new(shape, dtype, X, stream)
     _want(t, dtype, shape)
+    assert t.device == X.device, "tensors of different devices"
     return t
 
 

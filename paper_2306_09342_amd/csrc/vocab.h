@@ -58,8 +58,9 @@ struct VocabGemm {
     int piece, span;                // piece: its number; span: its width in the forward pass, a multiple of 256
     int losses;                     // whose exponentials without `dual`: LOSS_CE, LOSS_KD or both (tau = 1)
     float inv_tau;
+    double work;                    // of a product over a piece, for the timing of kernel families
 };
-// x = p[0] + p[1] + p[2] to 2^-25 of |x|; an infinity or NaN is p[0] alone.
+// x = p[0] + p[1] + p[2] to 2^-25 of |x|; an infinity (also of a value beyond the largest bf16, 3.39e38) or NaN is p[0] alone.
 __device__ __forceinline__ void split3(float x, bf16 (&p)[3]) {
     p[0] = from_f<bf16>(x);
     const float r = x - to_f(p[0]);

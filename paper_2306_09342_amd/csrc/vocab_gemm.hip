@@ -556,7 +556,7 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
         for (int kt = 0; kt < nst; ++kt) {
             if (kt + 1 < nst) wait_vm<8>();
             else wait_vm<0>();
-            __builtin_amdgcn_s_barrier();                          // everybody's loads of this stage have landed
+            asm volatile("s_barrier" ::: "memory");                // everybody's loads of this stage have landed
             const unsigned char* at = smem + (kt & 1) * VM_STAGE;
             bf16x8_t bf[4][2], af[4][2];
 #pragma unroll
@@ -569,7 +569,7 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
                 }
             }
             wait_lds();
-            __builtin_amdgcn_s_barrier();                          // and has been read
+            asm volatile("s_barrier" ::: "memory");                // and it has been read
             if (kt + 2 < nst) issue(kt + 2);
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk)
@@ -864,7 +864,7 @@ template <typename T> constexpr int parts_of = sizeof(T) == 2 ? 1 : 3;
 template <typename T>
 int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, bool mid, int64_t blocks) {
     constexpr int P = parts_of<T>;
-    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D);
+    ProfScope ps(K_VOCAB, s, p.work);
     const int64_t large = std::min<int64_t>(blocks, 256);          // one per CU
 #define FORM(G, U) if (grad == G && dual == U) {                                                                          \
         static LdsLimit lim[2];                                                                                          \
@@ -882,10 +882,10 @@ int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int*
     REV_HIP(hipGetLastError());
     return REV_OK;
 }
-// dx_blocks, dw_blocks: multiples of 8, most that there may be; 0: not wanted
+// dx_blocks (a multiple of 8: the tiles of dW begin on the first XCD), dw_blocks: most that there may be; 0: not wanted
 template <typename T>
 int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db) {
-    ProfScope ps(K_VOCAB, s, 2.0 * p.Mp * p.V * p.D * ((dx_blocks > 0) + (dw_blocks > 0)));
+    ProfScope ps(K_VOCAB, s, p.work * ((dx_blocks > 0) + (dw_blocks > 0)));
     static LdsLimit lim[2];
     const int first = (int)dx_blocks;
     if constexpr (sizeof(T) == 2)

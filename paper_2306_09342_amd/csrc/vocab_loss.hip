@@ -680,6 +680,11 @@ struct VocabRunner {
                     piece + 1 == pieces);
         return REV_OK;
     }
+    template <typename U, int P> int sparse_dz(int v0, int n, U* dz, int64_t ld, int64_t part) {
+        ProfScope ps(K_CONVERT, s, 4.0 * M * (v.K + 1));
+        LAUNCH((sparse_dz_kernel<U, P>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), v0, n, dz, ld, part);
+        return REV_OK;
+    }
     FewRows<T> few_args() {
         FewRows<T> f = {};
         f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
@@ -713,6 +718,7 @@ struct VocabRunner {
         g.span = L.span;
         for (int k = 0; k < pieces; ++k) {
             g.piece = k;
+            g.work = 2.0 * M * D * std::min<int64_t>(L.span, V - (int64_t)k * L.span);
             RC(vocab_logits<T>(s, g, false, dual(), L.mid, L.Mp / 256 * (L.span / 256)));
             RC(join(out, k, pieces));
         }
@@ -723,6 +729,7 @@ struct VocabRunner {
         RC(gemm_args(&g));
         FewRows<T> f = few_args();
         f.tile_dz = at<bf16>(L.dz);
+        g.work = 2.0 * M * D * V / L.pieces;                       // (how many of them there are is known to the device)
         f.rows_out = (int)up(M, 128);                              // dW goes over whole 128 rows
         for (int k = 0; k < L.pieces; ++k) {
             // tiles of 256 entries that piece k may have: there is a piece k only if a piece is at most a k+1-th of the vocabulary
@@ -730,8 +737,7 @@ struct VocabRunner {
             g.piece = k;
             if (L.few_dz) RC(few_logits<T>(s, f, true, false));
             else RC(vocab_logits<T>(s, g, true, dual(), L.mid, std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
-            if (v.idx) LAUNCH((sparse_dz_kernel<bf16, kParts>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), k, 0, at<bf16>(L.dz),
-                              (int64_t)0, L.lim.dz);
+            if (v.idx) RC((sparse_dz<bf16, kParts>(k, 0, at<bf16>(L.dz), 0, L.lim.dz)));
             RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) : 0, dparams,
                               c.grad_mode == REV_MODE_BF16, c.bias));
         }
@@ -742,7 +748,7 @@ struct VocabRunner {
     int backward_few(T* dX, void* dparams) {
         const FewRows<T> f = few_args();
         RC(few_logits<T>(s, f, true, false));
-        if (v.idx) LAUNCH((sparse_dz_kernel<float, 0>), blocks_of(M, 4), dim3(256), v, at<float>(L.zs), at<float4>(L.coef), 0, V, f.dz, f.ldz, (int64_t)0);
+        if (v.idx) RC((sparse_dz<float, 0>(0, V, f.dz, f.ldz, 0)));
         RC(few_grads<T>(s, f, dX != nullptr, dparams, c.grad_mode == REV_MODE_BF16, c.bias));
         return dX ? few_dx_rows<T>(s, f, v.place, dX) : REV_OK;
     }

@@ -347,6 +347,17 @@ def test_repeats_bit_for_bit_on_any_stream_and_two_at_once(mode):
             assert torch.equal(f[k], ref[k]), k
 
 
+@pytest.mark.parametrize("M,D,V", [(4, 64, 501), (300, 64, 700), (70001, 8, 45000)])
+def test_the_timing_of_kernel_families_counts_the_products_once(M, D, V):
+    c = VU.make(M, D, V, "bf16", K=2, seed=23)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    B.rev_profile_begin()
+    f = VU.forward(cfg, c, a)
+    VU.backward(cfg, c, a, f["stats"])
+    _, launches, work, is_flops = B.rev_profile_end()["vocab"]
+    assert work == pytest.approx(4 * 2.0 * M * D * V) and launches >= 3 and is_flops
+
+
 @pytest.mark.parametrize("mode", ["bf16", "fp32"])
 @pytest.mark.parametrize("M", [4, 300])
 def test_captured_and_replayed_with_other_inputs(M, mode):
