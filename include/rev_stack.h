@@ -380,22 +380,34 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * entry kd = lse_tau = 0; a row with neither takes no part: its dX is 0, and
  * X and the cotangents may hold anything there, infinities and NaN included.
  * A bias of -infinity, or of the type's lowest value, takes an entry out of
- * the vocabulary.  If no row counts, dparams is 0.
+ * the vocabulary; one entry has to stay.  Teacher logits may be the lowest
+ * value.  An infinity or NaN elsewhere in a row that counts gives NaN where the
+ * formulas do, in that row and in dparams.  If no row counts, dparams is 0.
  *
  * Types.  REV_MODE_FP32: everything float32.  REV_MODE_BF16: params, X and dX
  * bfloat16; dparams float32 or bfloat16 (cfg.grad_mode).  Logits, softmax
  * statistics and all sums are float32 in both modes; in bf16 mode dz is rounded
- * to bfloat16 once, as an operand of the two products.  loss, lse, dloss and
- * teacher_logits float32; labels and teacher_idx int32.
+ * to bfloat16 once, as an operand of the two products (for few rows not at
+ * all).  In float32 mode the products of more than a few rows take every operand
+ * as a sum of three bfloat16 values, which leaves out 2^-23 of |x||w| of a
+ * product; there, an infinite weight, or one beyond 3.39e38, gives NaN in its
+ * entry's logits where float32 would have an infinity.  loss, lse, dloss and
+ * teacher_logits are float32, labels and teacher_idx int32.
+ *
+ * Workspace.  A copy of the rows that count, and of W in float32 mode or if
+ * d_model % 128 != 0 (both go with the number of elements); a piece's dz, at most
+ * 512 MB, or 256 entries of all rows if that is more; its statistics, at most
+ * 256 MB likewise; fragments of dX in float32.  It does not grow with
+ * rows * vocab beyond these.
  *
  * Packed parameters: W[vocab, d_model] row-major, then b[vocab] if cfg.bias.
  * dparams: same layout, overwritten.  X, dX: [rows, d_model]; labels, loss,
  * dloss: [rows]; teacher_idx, teacher_logits: [rows, top_k].  All device
  * pointers; params, X, dX, dparams 16-byte aligned, the others 4-byte; the
  * workspace 256-byte aligned and at least rev_vocab_workspace_bytes() long.
- * Calls enqueue on `stream` and return; nothing is allocated, every region of
- * the workspace is written before it is read, and calls may be captured into
- * a HIP graph.  Sums have a fixed order; a row's loss and dX do not depend on
+ * Calls enqueue on `stream` and return; nothing is allocated, the workspace may
+ * hold anything before a call and is free for others after it, and calls may be
+ * captured into a HIP graph.  Sums have a fixed order; a row's loss and dX do not depend on
  * the rows beside it as long as cfg.rows and the number of rows that count stay
  * the same.
  *
