@@ -38,8 +38,6 @@ __device__ __forceinline__ Piece piece_of(int k, int width, int V) {
     return {(int)v0, v0 < V ? min(width, V - (int)v0) : 0};
 }
 
-struct LabelDz { int label; float dz; };         // a row's label, and dz there
-
 constexpr int LOSS_CE = 1, LOSS_KD = 2;
 // The products (vocab_gemm.hip).  bf16 operands are one part; a float32 one is the sum of three bf16 parts (split3).
 struct VocabGemm {
@@ -50,7 +48,7 @@ struct VocabGemm {
     const void* bias;               // [V] or null, bf16, or float32 with three parts
     float* stats;                   // forward: [half tiles][maximum, sum of exp(z - maximum), ...][Mp]; see vocab_logits_kernel
     const float4* coef;             // backward: of every row that counts (dense_dz)
-    const LabelDz* label_dz;        // of every row that counts, where labels alone are named, or null
+    const int* label;               // of every row that counts, where labels alone are named, or null
     bf16* dz;                       // a part [rows, width] of a piece
     float* acc;                     // dx, 65536 floats per tile and range
     int64_t Mp, dz_part;            // dz_part: elements from a part of dz to the next
@@ -82,7 +80,7 @@ template <typename T> struct FewRows {
     const T* bias;                  // [V] or null
     float* stats;                   // as VocabGemm::stats, of strips of 64 entries: row i at i stat_row, kinds stat_kind apart
     const float4* coef;
-    const LabelDz* label_dz;
+    const int* label;
     float* dz;                      // [rows_out, ldz], zeros behind the rows that count and the vocabulary
     bf16* tile_dz;                  // the same in bf16, for the products of tiles, in the plan's width; or null
     float* parts;                   // dx of a range of the vocabulary, [range][rows][D]

@@ -149,17 +149,17 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
         }
     } else {
         float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
-        LabelDz y = {-1, 0.f};
+        int y = -1;
         if (i < count) {
             c = p.coef[i];
-            if (p.label_dz) y = p.label_dz[i];
+            if (p.label) y = p.label[i];
         }
         const int64_t ldz = p.tile_dz ? pl.width : p.ldz;
         float d[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
             d[e] = i < count && c0 + e < p.V ? dense_dz(c, z[e], p.inv_tau) : 0.f;
-            if (c0 + e == y.label) d[e] = y.dz;
+            if (c0 + e == y) d[e] -= c.x;
         }
 #pragma unroll
         for (int e = 0; e < EPT; e += 4) {

@@ -278,9 +278,9 @@ __device__ __forceinline__ void row_stats(const f32x16_t (&z)[N], float e0, floa
 }
 
 // dz of 16 entries of a row, those of lane g of 32, from its coefficients (without DUAL: the one exponential's; both losses have the
-// same at tau = 1), with the label's, entry `at` of the lane's, in its place; to `out`, where lane g's first eight of them go.
+// same at tau = 1), less the row's weight at its label, entry `at` of the lane's; to `out`, where lane g's first eight of them go.
 template <bool DUAL, int P>
-__device__ __forceinline__ void dz_block(const f32x16_t& z, const float4& c, float rate0, float inv_tau, int at, float label_dz, bf16* out, int64_t part_dz) {
+__device__ __forceinline__ void dz_block(const f32x16_t& z, const float4& c, float rate0, float inv_tau, int at, bf16* out, int64_t part_dz) {
     f32x16_t d;
 #pragma unroll
     for (int v = 0; v < 16; ++v) {
@@ -290,7 +290,7 @@ __device__ __forceinline__ void dz_block(const f32x16_t& z, const float4& c, flo
     if (__any((unsigned)at < 28u)) {
 #pragma unroll
         for (int v = 0; v < 16; ++v)
-            if (at == 8 * (v >> 2) + (v & 3)) d[v] = label_dz;
+            if (at == 8 * (v >> 2) + (v & 3)) d[v] -= c.x;
     }
 #pragma unroll
     for (int part = 0; part < P; ++part) {
@@ -324,7 +324,7 @@ __device__ __forceinline__ void start_at_end(f32x16_t& z, int c0, int n, int par
 // The logits of tiles of 256 rows and 256 entries.  The accumulators start at the bias, and at -infinity beyond the vocabulary, so
 // that neither costs the epilogue anything.  An accumulator's lane has one row of X in each half and 64 entries of it.  Forward: the
 // sums are of exp(z - maximum), or exp((z - maximum) / tau) if only the teacher's loss is wanted; with DUAL the two are
-// kept side by side.  Backward: dz, with the label's entry in its place where labels alone are named.
+// kept side by side.  Backward: dz, its label's entry p - 1 before it is rounded where labels alone are named.
 // What bounds it: see the file's head; the epilogue is 128 exponentials a lane (twice that with DUAL).  The first two stages
 // of the next tile are under way meanwhile, and its bias.
 template <bool GRAD, bool DUAL, int P>
@@ -349,8 +349,7 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
     int m0, n0;
     const char *a_base, *b_base;
     unsigned vb[2][2];
-    // The rest goes to 2 KB of LDS of the wavefront's own: the bias of its 2 x 64 entries, {coefficients, label, dz there} of its 2 x 32
-    // rows.  (Registers for it would be short of 20 in the main loop.)
+    // The rest goes to 2 KB of LDS of the wavefront's own: the bias of its 2 x 64 entries, coefficients and label of its 2 x 32 rows.  (Registers for it would be short of 20 in the main loop.)
     typedef typename std::conditional<P == 1, u32x2_t, f32x4_t>::type quad_t;
     unsigned char* side = smem + VG_LDS + t.wave * VG_SIDE;
     const unsigned side_lds = (unsigned)(uintptr_t)LDS_PTR(unsigned char, side);
@@ -378,10 +377,7 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
         if (GRAD) {
             const int row = m0 + (t.lane >> 5) * 128 + t.wn * 32 + t.fr;
             dma16_sbase(p.coef, row * 16, side_lds + 512);
-            if (p.label_dz) {
-                dma4_sbase(p.label_dz, row * 8, side_lds + 1536);
-                dma4_sbase(p.label_dz, row * 8 + 4, side_lds + 1792);
-            }
+            if (p.label) dma4_sbase(p.label, row * 4, side_lds + 1536);
         }
     };
     auto issue_a = [&](auto half, int kt, unsigned lds) {
@@ -432,17 +428,16 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
         const int tm0 = m0, tn0 = n0;
         tile_products<false, false>(smem, t, issue_a, issue_b, parts.total(), acc);
         float4 tc[2];
-        LabelDz ty[2];
+        int ty[2];
         if (GRAD) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 // rows behind the last one that counts: 0 exp(z - infinity)
                 tc[j] = make_float4(0.f, INFINITY, 0.f, INFINITY);
-                ty[j] = {-1, 0.f};
+                ty[j] = -1;
                 if (tm0 + j * 128 + t.wn * 32 + t.fr < pl.count) {
                     tc[j] = *reinterpret_cast<const float4*>(side + 512 + (j * 32 + t.fr) * 16);
-                    if (p.label_dz) ty[j] = {*reinterpret_cast<const int*>(side + 1536 + (j * 32 + t.fr) * 4),
-                                             *reinterpret_cast<const float*>(side + 1792 + (j * 32 + t.fr) * 4)};
+                    if (p.label) ty[j] = *reinterpret_cast<const int*>(side + 1536 + (j * 32 + t.fr) * 4);
                 }
             }
             wait_lds();                                            // the next tile's take their place
@@ -471,12 +466,12 @@ __global__ __launch_bounds__(512, 2) void vocab_logits_kernel(VocabGemm p) {
                 const int64_t row = tm0 + j * 128 + t.wn * 32 + t.fr;
                 if (row - t.fr >= dz_rows) continue;
                 bf16* out = p.dz + row * width + tn0 + t.wm * 64 + 8 * t.g;
-                const int at = ty[j].label - (v0 + tn0 + t.wm * 64 + 4 * t.g);
+                const int at = ty[j] - (v0 + tn0 + t.wm * 64 + 4 * t.g);
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
-                        dz_block<DUAL, P>(acc[h][j][i], c, rate0, p.inv_tau, at - h * 128 - i * 32, ty[j].dz, out + h * 128 + i * 32, p.dz_part);
+                        dz_block<DUAL, P>(acc[h][j][i], c, rate0, p.inv_tau, at - h * 128 - i * 32, out + h * 128 + i * 32, p.dz_part);
             }
         }
         if (!more) break;
@@ -593,16 +588,16 @@ __global__ __launch_bounds__(256, 2) void vocab_logits_mid_kernel(VocabGemm p) {
         for (int j = 0; j < 2; ++j) {
             const int64_t row = m0 + wn * 64 + j * 32 + fr;
             float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);  // rows behind the last one that counts: 0 exp(z - infinity)
-            LabelDz y = {-1, 0.f};
+            int y = -1;
             if (row < pl.count) {
                 c = p.coef[row];
-                if (p.label_dz) y = p.label_dz[row];
+                if (p.label) y = p.label[row];
             }
             if (!DUAL) c = one_coef(c, p.losses);
             bf16* out = p.dz + row * width + n0 + wm * 64 + 8 * g;
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                dz_block<DUAL, P>(acc[i][j], c, rate0, p.inv_tau, y.label - (v0 + n0 + wm * 64 + 4 * g) - i * 32, y.dz, out + i * 32, p.dz_part);
+                dz_block<DUAL, P>(acc[i][j], c, rate0, p.inv_tau, y - (v0 + n0 + wm * 64 + 4 * g) - i * 32, out + i * 32, p.dz_part);
         }
     }
 }

@@ -3,9 +3,9 @@
 //
 // Both losses have the gradient   dz = c0 exp(z - lse) + c1 exp(z / tau - lse_tau)   at every entry of the vocabulary, and
 // something to be subtracted at the few entries that a row's label and teacher name.  The products compute the dense part only; the
-// logits at the named entries are dot products of their own (sparse_logits_kernel: a row of W per entry), the losses
-// are made of them, and in the backward pass the entries of dz that they touch are written again, from float32, behind the
-// dense part (sparse_dz_kernel), so that p - 1 and q - p are rounded once and not taken from a rounded p.
+// logits at the named entries are dot products of their own (gather_row: a row of W per entry), the losses are made of them, and in
+// the backward pass the entries of dz that a teacher touches are written again, from float32, behind the dense part
+// (sparse_dz_kernel), so that q - p is rounded once and not taken from a rounded q.  p - 1 at a label alone the products see to.
 //
 // Rows that do not count (no label, no teacher) are left out before anything is multiplied: the others are gathered to the
 // front of a copy of X, in their order, with rows of zeros behind them.  Their number stays on the device.
@@ -160,8 +160,9 @@ __device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
 }
 
 // Row i of Xc = row r of X, padded with zeros to Dp columns, all zeros beyond the last row that counts; zs[i][e] = <W_v, x> + b_v for its
-// entries, a wavefront of the workgroup per entry at a time; in the backward pass also what the row's dense part is made of, and
-// dz at its label, which without a teacher is all that is named.  P: bf16 parts that the copy has, 0: its own type.
+// entries, a wavefront of the workgroup per entry at a time; in the backward pass also what the row's dense part is made of.  Without
+// a teacher the products find dz at the label by themselves: the label goes with the row, and its logit is not wanted.  P: bf16 parts
+// that the copy has, 0: its own type.
 struct Cotangents { const float *lse, *lse_tau, *dce, *dkd; };
 template <typename T> struct GatherArgs {
     const T* params; const T* X;
@@ -171,7 +172,7 @@ template <typename T> struct GatherArgs {
     float* zs;
     Cotangents cot;
     float4* coef;
-    LabelDz* label_dz;
+    int* label;
 };
 template <typename T, int P>
 __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<T>& g, int i, bool live, int r, int flags) {
@@ -184,11 +185,15 @@ __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<
         else store_parts(u, reinterpret_cast<bf16*>(g.Xc) + (int64_t)i * g.Dp + d, g.Mp * g.Dp);
     }
     if (!live) return;
-    float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
-    if (g.coef) {
+    if (g.coef && threadIdx.x == 0) {
+        float4 c = make_float4(0.f, INFINITY, 0.f, INFINITY);
         if (flags & HAS_LABEL) { c.x = g.cot.dce[r]; c.y = g.cot.lse[r]; }
         if (flags & HAS_TEACHER) { c.z = g.cot.dkd[r] / v.inv_tau; c.w = g.cot.lse_tau[r]; }
-        if (threadIdx.x == 0) g.coef[i] = c;
+        g.coef[i] = c;
+    }
+    if (g.label) {
+        if (threadIdx.x == 0) g.label[i] = entry_of(v, r, 0);
+        return;
     }
     // four entries of a wavefront at a time, so that four rows of W are under way
     const int lane = threadIdx.x & 63;
@@ -225,7 +230,6 @@ __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<
             float z = wave_sum(sum[u]);
             if (n[u] >= 0 && v.bias) z += to_f(g.params[(int64_t)v.V * g.D + n[u]]);
             if (lane == 0) g.zs[(int64_t)i * (v.K + 1) + e0 + u] = z;
-            if (e0 + u == 0 && lane == 0 && g.label_dz) g.label_dz[i] = {n[u], dense_dz(c, z, v.inv_tau) - c.x};
         }
     }
 }
@@ -569,7 +573,7 @@ constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 // the statistics of a piece in the forward pass, three per 128 entries of a row, or those of 256 entries if that is more
 constexpr int64_t VOCAB_STATS_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, label_dz, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, total;
+    int64_t plan, flags, place, list, coef, label, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, total;
     int64_t Mp, ldz;                 // ldz: of dz in float32
     bool few_f, few_b, few_dz, mid;  // few rows: forward, backward, dz alone; tiles of 128
     int parts;                       // bf16 parts of an operand of the products of tiles
@@ -599,7 +603,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
     L.place = take(4 * M);
     L.list = take(4 * M);
     L.coef = take(16 * L.Mp);
-    L.label_dz = take(8 * L.Mp);
+    L.label = take(4 * L.Mp);
     L.zs = take(4 * M * (c.top_k + 1));
     L.stats = take(12 * (L.few_f ? M : L.Mp) * L.strips);
     if (large) L.carry = take(12 * L.Mp);
@@ -656,7 +660,7 @@ struct VocabRunner {
     template <int P> int prepare(const void* X, const RowResults& zero, const Cotangents& cot) {
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
         const GatherArgs<T> g = {params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), cot, cot.lse ? at<float4>(L.coef) : nullptr,
-                                 cot.lse && !v.idx ? at<LabelDz>(L.label_dz) : nullptr};
+                                 cot.lse && !v.idx ? at<int>(L.label) : nullptr};
         const dim3 rows((unsigned)L.Mp), block(256);
         if (M <= SELECT_ROWS && (int64_t)M * (v.K + 1) <= SELECT_ENTRIES) {
             LAUNCH((select_gather_kernel<T, P>), rows, block, v, g, at<uint8_t>(L.flags), at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
@@ -688,7 +692,7 @@ struct VocabRunner {
     FewRows<T> few_args() {
         FewRows<T> f = {};
         f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
-        f.label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
+        f.label = v.idx ? nullptr : at<int>(L.label); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
         f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
         f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = f.rows_out = M;
         f.range = L.range; f.ranges = L.ranges; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
@@ -698,7 +702,7 @@ struct VocabRunner {
     // ---- products of bf16 parts ----
     int gemm_args(VocabGemm* g) {
         *g = {};
-        g->plan = v.plan; g->x = at<bf16>(L.xc); g->bias = bias(); g->label_dz = v.idx ? nullptr : at<LabelDz>(L.label_dz);
+        g->plan = v.plan; g->x = at<bf16>(L.xc); g->bias = bias(); g->label = v.idx ? nullptr : at<int>(L.label);
         g->stats = at<float>(L.stats); g->coef = at<float4>(L.coef); g->dz = at<bf16>(L.dz); g->acc = at<float>(L.acc);
         g->Mp = L.Mp; g->dz_part = L.lim.dz; g->V = V; g->D = D; g->Dp = L.Dp; g->losses = losses(); g->inv_tau = v.inv_tau;
         g->w = g->wp = (const bf16*)params;
