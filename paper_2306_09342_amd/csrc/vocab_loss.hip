@@ -16,22 +16,30 @@
 
 namespace rev {
 
-// What bounds a plan: floats of dz, tiles of 256 columns in dx, places for its ranges (0, 0, 0: the float32 products, which have none).
-struct PlanLimits { int64_t dz; int tiles_d, slots; };
+// What bounds a plan: floats of dz, tiles of 256 columns in dx, places for its ranges (0, 0, 0: there are no tiles); products of
+// parts that make one; whether dW is wanted.
+struct PlanLimits { int64_t dz; int tiles_d, slots, terms, dw; };
 struct RowResults { float* p[4]; };
 
-// Pieces of equal widths whose dz fits.  dx has few tiles: its contraction, the piece, is cut into the number of ranges that keeps the
-// 256 CUs busiest; a range costs about 10 stages besides its own (first loads, and writing and reading 256 KB).  By one wavefront,
-// a number of ranges per lane.
+// Pieces of equal widths whose dz fits.  dx has few tiles: its contraction, the piece, is cut into ranges.  A tile or range costs about
+// 10 stages besides its own (first loads, and writing and reading 256 KB), and a stage of dx 4/3 of one of dW, which goes along rows.  Alone,
+// dx has the number of ranges that keeps the 256 CUs busiest; beside dW, whose tiles fill the CUs that it leaves, the smallest that
+// lets its workgroups end before the whole does.  By one wavefront, a number of ranges per lane.
 __device__ __forceinline__ void write_plan(int count, int V, const PlanLimits& lim, VocabPlan* __restrict__ plan, int lane) {
     VocabPlan p = {count, (count + 255) / 256 * 256, (V + 255) / 256 * 256, 1, 2};
     if (lim.dz != 0 && count != 0) {                               // (without rows: one piece of zeros for dW)
         const unsigned most = (unsigned)((lim.dz / 256) / (p.rows / 256) / 256 * 256), pieces = (V + most - 1) / most;
         p.width = (int)((V + pieces - 1) / pieces + 255) / 256 * 256;
         const int tiles = p.rows / 256 * lim.tiles_d, pairs = p.width / 128, s = lane + 1;
-        const int stages = (pairs + s - 1) / s * 2;
-        // a range of a tile is read once more
-        unsigned cost = s <= pairs && tiles * s <= lim.slots ? (unsigned)((tiles * s + 255) / 256) * (stages + 10) * 2 + s : ~0u;
+        const int stages = (pairs + s - 1) / s * 2, terms = lim.terms;
+        unsigned cost = ~0u;                                       // in 768ths of a stage of dW
+        if (s <= pairs && tiles * s <= lim.slots) {
+            cost = (unsigned)((tiles * s + 255) / 256) * (terms * stages + 10) * 1024 + s;
+            if (lim.dw) {
+                const unsigned tile = terms * (p.rows / 64) + 10, all = 4 * tiles * (terms * pairs * 2 + 10 * s) + 3 * (p.width / 256) * lim.tiles_d * tile;
+                cost = max(cost, all + 384 * tile);                // half a tile of dW idle at the end
+            }
+        }
         unsigned best = cost;
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) best = min(best, (unsigned)__shfl_xor((int)best, o, 64));
@@ -614,6 +622,7 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
         const int64_t all = L.Mp * up(V, 256);
         L.lim.dz = L.few_dz ? all : std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
         L.lim.tiles_d = (int)((D + 255) / 256);
+        L.lim.terms = L.parts == 1 ? 1 : 6;
         L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
         L.pieces = (int)((V + least - 1) / least);
@@ -657,17 +666,19 @@ struct VocabRunner {
     bool dual() const { return losses() == (LOSS_CE | LOSS_KD) && c.temperature != 1.f; }
 
     // the rows that count, their logits at named entries, and in the backward pass (cot.lse) what their dense parts are made of
-    template <int P> int prepare(const void* X, const RowResults& zero, const Cotangents& cot) {
+    template <int P> int prepare(const void* X, const RowResults& zero, const Cotangents& cot, bool dw = false) {
+        PlanLimits lim = L.lim;
+        lim.dw = dw;
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
         const GatherArgs<T> g = {params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), cot, cot.lse ? at<float4>(L.coef) : nullptr,
                                  cot.lse && !v.idx ? at<int>(L.label) : nullptr};
         const dim3 rows((unsigned)L.Mp), block(256);
         if (M <= SELECT_ROWS && (int64_t)M * (v.K + 1) <= SELECT_ENTRIES) {
-            LAUNCH((select_gather_kernel<T, P>), rows, block, v, g, at<uint8_t>(L.flags), at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
+            LAUNCH((select_gather_kernel<T, P>), rows, block, v, g, at<uint8_t>(L.flags), at<int>(L.list), at<int>(L.place), zero, lim, at<VocabPlan>(L.plan));
             return REV_OK;
         }
         if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
-        LAUNCH(select_rows_kernel, dim3(SELECT_BLOCKS), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, L.lim, at<VocabPlan>(L.plan));
+        LAUNCH(select_rows_kernel, dim3(SELECT_BLOCKS), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, lim, at<VocabPlan>(L.plan));
         LAUNCH((gather_kernel<T, P>), rows, block, v, g, flags());
         return REV_OK;
     }
@@ -768,7 +779,7 @@ struct VocabRunner {
     }
     int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
         if (!L.few_b) {
-            RC(prepare<kParts>(X, RowResults{}, cot));
+            RC(prepare<kParts>(X, RowResults{}, cot, dparams != nullptr));
             return backward_parts((T*)dX, dparams);
         }
         RC(prepare<0>(X, RowResults{}, cot));
