@@ -1,6 +1,7 @@
 // What the files of the losses over a vocabulary share.
 #pragma once
 #include "common.h"
+#include "rowwise.h"
 
 namespace rev {
 
@@ -22,6 +23,58 @@ struct VocabRows {
     float inv_tau;
 };
 
+constexpr int LOSS_CE = 1, LOSS_KD = 2, HAS_LABEL = LOSS_CE, HAS_TEACHER = LOSS_KD;
+__device__ __forceinline__ bool in_vocab(int v, int V) { return (unsigned)v < (unsigned)V; }
+__device__ __forceinline__ bool teacher_counts(int idx, float logit, int V) { return in_vocab(idx, V) && !(logit == -INFINITY); }
+// Entry 0 of a row is its label, entries 1 .. K its teacher's; -1: none.
+__device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
+    if (e == 0) {
+        const int y = v.labels ? v.labels[r] : -1;
+        return in_vocab(y, v.V) ? y : -1;
+    }
+    const int64_t at = (int64_t)r * v.K + e - 1;
+    return teacher_counts(v.idx[at], v.logits[at], v.V) ? v.idx[at] : -1;
+}
+// z[e] = <W_n, x> + b_n for up to four entries n of row r from e0 on, by a wavefront: four rows of W are under way.
+template <typename T>
+__device__ __forceinline__ void named_logits(const VocabRows& v, const T* x, const T* params, int D, int r, int e0, float* z) {
+    constexpr int E = 16 / sizeof(T);
+    const int lane = threadIdx.x & 63;
+    int n[4];
+    const T* w[4];
+    float sum[4] = {};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        n[u] = e0 + u <= v.K ? entry_of(v, r, e0 + u) : -1;
+        w[u] = params + (int64_t)max(n[u], 0) * D;
+    }
+    for (int d = lane * E; d < D; d += 64 * E) {
+        f4 a[E / 4];
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) a[q] = load4(x + d + 4 * q);
+        uint4 b[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) b[u] = n[u] >= 0 ? *reinterpret_cast<const uint4*>(w[u] + d) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const T* f = reinterpret_cast<const T*>(&b[u]);
+#pragma unroll
+            for (int q = 0; q < E / 4; ++q) {
+                const f4 c = load4(f + 4 * q);
+                sum[u] = fmaf(a[q].x, c.x, sum[u]); sum[u] = fmaf(a[q].y, c.y, sum[u]);
+                sum[u] = fmaf(a[q].z, c.z, sum[u]); sum[u] = fmaf(a[q].w, c.w, sum[u]);
+            }
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        if (e0 + u > v.K) break;
+        float s = wave_sum(sum[u]);
+        if (n[u] >= 0 && v.bias) s += to_f(params[(int64_t)v.V * D + n[u]]);
+        if (lane == 0) z[e0 + u] = s;
+    }
+}
+
 // The dense part of a row's dz at a logit z: c = {dloss_ce, lse, dloss tau, lse_tau}, {0, infinity} where the row has none.
 __device__ __forceinline__ float dense_dz(const float4& c, float z, float inv_tau) {
     float d = 0.f;
@@ -38,7 +91,6 @@ __device__ __forceinline__ Piece piece_of(int k, int width, int V) {
     return {(int)v0, v0 < V ? min(width, V - (int)v0) : 0};
 }
 
-constexpr int LOSS_CE = 1, LOSS_KD = 2;
 // The products (vocab_gemm.hip).  bf16 operands are one part; a float32 one is the sum of three bf16 parts (split3).
 struct VocabGemm {
     const VocabPlan* plan;
@@ -72,12 +124,15 @@ template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool g
 template <typename T> int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db);
 template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX);
 
-// Few rows (vocab_few.hip): the statistics of the logits, or dz of the whole vocabulary in float32, and the gradients from that.
+// Few rows (vocab_few.hip): the statistics of the logits of all rows and the logits that they name; or dz of the whole vocabulary in
+// float32, of the rows that count, and the gradients from that.
 template <typename T> struct FewRows {
-    const VocabPlan* plan;
-    const T* x;                     // rows that count, [rows_x, Dp], zeros behind them
+    const VocabPlan* plan;          // null forward
+    const T* x;                     // forward X; backward the rows that count, [rows_x, ldx], zeros behind them
     const T* w;                     // [V, D]
     const T* bias;                  // [V] or null
+    VocabRows named;                // forward: whose logits go to
+    float* zs;                      // [rows][K + 1]
     float* stats;                   // as VocabGemm::stats, of strips of 64 entries: row i at i stat_row, kinds stat_kind apart
     const float4* coef;
     const int* label;
@@ -85,7 +140,8 @@ template <typename T> struct FewRows {
     bf16* tile_dz;                  // the same in bf16, for the products of tiles, in the plan's width; or null
     float* parts;                   // dx of a range of the vocabulary, [range][rows][D]
     int64_t stat_row, stat_kind, ldz;
-    int V, D, Dp, losses, rows_x, rows, rows_out, blocks_m;    // rows: most that count
+    int V, D, ldx, losses, rows_x, rows, rows_out, blocks_m;    // rows: most that count
+    int named_blocks;               // workgroups for the named logits, a multiple of 8
     int range, ranges, col_groups;  // entries per range, a multiple of 32
     float inv_tau;
 };

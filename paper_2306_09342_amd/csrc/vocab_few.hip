@@ -6,6 +6,10 @@
 // which the softmax statistics or dz are made of.  (Both operands read straight into registers instead: every lane of such a load is
 // in another row, and the address unit took 12 us for 64 rows and 1000 entries of 768, 31 for one row and 50265.)
 //
+// Forward the rows are taken from X as they lie, those that do not count too (their results are not kept): nothing has to be selected first,
+// and the logits that the rows name are dot products in workgroups ahead of the others.  (Selected, copied and their named logits
+// taken by a launch of its own: 26 us for one row and 41 for 16 rows with 8 named entries each, in the place of 20 and 29.)
+//
 // What bounds it: reading W.  One row of 768, 50265 entries, bf16 (77 MB): 19 us, 4.1 TB/s; 16 rows of 1024 (103 MB): 22 us.
 #include "mfma.h"
 #include "vocab.h"
@@ -37,12 +41,15 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
     constexpr int NB = 2, ROWS = C::ROWS, PITCH = C::PITCH, NS = C::STAGES, LOADS = C::LOADS, TPR = 256 / ROWS, EPT = 64 / TPR;
     extern __shared__ __attribute__((aligned(1024))) unsigned char smem[];
     float* red = reinterpret_cast<float*>(smem);
-    const VocabPlan pl = *p.plan;
     const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tile = xcd_remap(blockIdx.x, gridDim.x), nt = tile / p.blocks_m, m0 = (tile - nt * p.blocks_m) * ROWS, n0 = nt * 64;
-    if (!GRAD && m0 >= pl.count) return;
-    const int count = pl.count;
+    if (!GRAD && (int)blockIdx.x < p.named_blocks) {               // four named entries of a row per wavefront
+        const int per = (p.named.K + 4) >> 2, item = blockIdx.x * 4 + wave, r = item / per;
+        if (r < p.rows) named_logits(p.named, p.x + (int64_t)r * p.ldx, p.w, p.D, r, (item - r * per) * 4, p.zs + (int64_t)r * (p.named.K + 1));
+        return;
+    }
+    const int ahead = GRAD ? 0 : p.named_blocks, tile = xcd_remap(blockIdx.x - ahead, gridDim.x - ahead), nt = tile / p.blocks_m, m0 = (tile - nt * p.blocks_m) * ROWS, n0 = nt * 64;
+    const int count = GRAD ? p.plan->count : p.rows;
 
     f32x16_t acc[NB][MB];
 #pragma unroll
@@ -57,7 +64,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
         const int units = p.D * (int)sizeof(T) / 16, lr = lane >> 2, unit = (lane & 3) ^ ((lr >> 1) & 3);
         const char* src[LOADS];
 #pragma unroll
-        for (int t = 0; t < 2 * MB; ++t) src[t] = reinterpret_cast<const char*>(p.x + (int64_t)min(m0 + 16 * t + lr, p.rows_x - 1) * p.Dp) + unit * 16;
+        for (int t = 0; t < 2 * MB; ++t) src[t] = reinterpret_cast<const char*>(p.x + (int64_t)min(m0 + 16 * t + lr, p.rows_x - 1) * p.ldx) + unit * 16;
 #pragma unroll
         for (int t = 0; t < 4; ++t) src[2 * MB + t] = reinterpret_cast<const char*>(p.w + (int64_t)min(n0 + 16 * t + lr, p.V - 1) * p.D) + unit * 16;
         unsigned char* ring = smem + wave * NS * C::STAGE;
@@ -154,7 +161,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
             c = p.coef[i];
             if (p.label) y = p.label[i];
         }
-        const int64_t ldz = p.tile_dz ? pl.width : p.ldz;
+        const int64_t ldz = p.tile_dz ? p.plan->width : p.ldz;
         float d[EPT];
 #pragma unroll
         for (int e = 0; e < EPT; ++e) {
@@ -233,7 +240,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
         unsigned kept[KEPT];
         if (MB == 1 && dparams) {
 #pragma unroll
-            for (int s = 0; s < KEPT; ++s) kept[s] = 2 * s < count ? word(x + (int64_t)(2 * s + g) * p.Dp) : 0u;
+            for (int s = 0; s < KEPT; ++s) kept[s] = 2 * s < count ? word(x + (int64_t)(2 * s + g) * p.ldx) : 0u;
         }
         for (int vb = 0; vb < nv && dparams; vb += 32) {
             f32x16_t acc[CS];
@@ -254,7 +261,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
                 unsigned xv[8], next[8];
                 auto load = [&](unsigned (&to)[8], int s0) {
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.Dp);
+                    for (int s = 0; s < 8; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx);
                 };
                 load(next, 0);
                 for (int s0 = 0; 2 * s0 < count; s0 += 8) {
@@ -378,7 +385,8 @@ template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, boo
     const int tiles = grad && p.tile_dz ? (p.V + 255) / 256 * 4 : (p.V + 63) / 64, covered = grad ? p.rows_out : p.rows;
     const bool one = p.rows <= 32 || (int64_t)((p.rows + 31) / 32) * tiles <= 512;
     p.blocks_m = (covered + (one ? 31 : 63)) / (one ? 32 : 64);
-    const dim3 grid((unsigned)(p.blocks_m * tiles)), block(256);
+    p.named_blocks = grad ? 0 : (int)(((int64_t)p.rows * ((p.named.K + 4) >> 2) + 31) / 32 * 8);
+    const dim3 grid((unsigned)(p.named_blocks + p.blocks_m * tiles)), block(256);
 #define FEW1(G, U, MB) do {                                                                                          \
         static LdsLimit lim;                                                                                         \
         if (int rc = lim.ensure(reinterpret_cast<const void*>(few_logits_kernel<T, G, U, MB>), FewCfg<MB>::LDS)) return rc; \

@@ -53,19 +53,17 @@ __device__ __forceinline__ void write_plan(int count, int V, const PlanLimits& l
 // ---------------------------------------------------------------------------------
 // which rows count
 // ---------------------------------------------------------------------------------
-constexpr int HAS_LABEL = LOSS_CE, HAS_TEACHER = LOSS_KD;
-__device__ __forceinline__ bool in_vocab(int v, int V) { return (unsigned)v < (unsigned)V; }
-__device__ __forceinline__ bool teacher_counts(int idx, float logit, int V) { return in_vocab(idx, V) && !(logit == -INFINITY); }
-
-// One wavefront per row: whether it has a label and whether it has a teacher.
-__global__ __launch_bounds__(256) void row_flags_kernel(const int* __restrict__ labels, const int* __restrict__ idx,
-                                                        const float* __restrict__ logits, int M, int V, int K, uint8_t* __restrict__ flags) {
-    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r >= M) return;
+// Whether a row has a label and whether it has a teacher, by a wavefront.
+__device__ __forceinline__ int row_flags(const VocabRows& v, int r, int lane) {
     bool any = false;
-    for (int k = lane; k < K; k += 64) any |= teacher_counts(idx[(int64_t)r * K + k], logits[(int64_t)r * K + k], V);
-    const bool taught = __any(any);
-    if (lane == 0) flags[r] = (labels && in_vocab(labels[r], V) ? HAS_LABEL : 0) | (taught ? HAS_TEACHER : 0);
+    for (int k = lane; k < v.K; k += 64) any |= entry_of(v, r, k + 1) >= 0;
+    return (__any(any) ? HAS_TEACHER : 0) | (entry_of(v, r, 0) >= 0 ? HAS_LABEL : 0);
+}
+__global__ __launch_bounds__(256) void row_flags_kernel(VocabRows v, uint8_t* __restrict__ flags) {
+    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (r >= v.M) return;
+    const int f = row_flags(v, r, lane);
+    if (lane == 0) flags[r] = (uint8_t)f;
 }
 
 // list[i] = the i-th row that counts, place[r] = i or -1, zeros in the results of the others, and the plan.  16384 rows at a time, a
@@ -157,16 +155,6 @@ __global__ __launch_bounds__(256) void lay_out_kernel(const T* __restrict__ w, i
 // ---------------------------------------------------------------------------------
 // logits at the entries that a row names
 // ---------------------------------------------------------------------------------
-// Entry 0 of a row is its label, entries 1 .. K its teacher's; -1: none.
-__device__ __forceinline__ int entry_of(const VocabRows& v, int r, int e) {
-    if (e == 0) {
-        const int y = v.labels ? v.labels[r] : -1;
-        return in_vocab(y, v.V) ? y : -1;
-    }
-    const int64_t at = (int64_t)r * v.K + e - 1;
-    return teacher_counts(v.idx[at], v.logits[at], v.V) ? v.idx[at] : -1;
-}
-
 // Row i of Xc = row r of X, padded with zeros to Dp columns, all zeros beyond the last row that counts; zs[i][e] = <W_v, x> + b_v for its
 // entries, a wavefront of the workgroup per entry at a time; in the backward pass also what the row's dense part is made of.  Without
 // a teacher the products find dz at the label by themselves: the label goes with the row, and its logit is not wanted.  P: bf16 parts
@@ -203,43 +191,7 @@ __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<
         if (threadIdx.x == 0) g.label[i] = entry_of(v, r, 0);
         return;
     }
-    // four entries of a wavefront at a time, so that four rows of W are under way
-    const int lane = threadIdx.x & 63;
-    for (int e0 = (threadIdx.x >> 6) * 4; e0 <= v.K; e0 += 16) {
-        int n[4];
-        const T* w[4];
-        float sum[4] = {};
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            n[u] = e0 + u <= v.K ? entry_of(v, r, e0 + u) : -1;
-            w[u] = g.params + (int64_t)max(n[u], 0) * g.D;
-        }
-        for (int d = lane * E; d < g.D; d += 64 * E) {
-            f4 a[E / 4];
-#pragma unroll
-            for (int q = 0; q < E / 4; ++q) a[q] = load4(x + d + 4 * q);
-            uint4 b[4];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) b[u] = n[u] >= 0 ? *reinterpret_cast<const uint4*>(w[u] + d) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const T* f = reinterpret_cast<const T*>(&b[u]);
-#pragma unroll
-                for (int q = 0; q < E / 4; ++q) {
-                    const f4 c = load4(f + 4 * q);
-                    sum[u] = fmaf(a[q].x, c.x, sum[u]); sum[u] = fmaf(a[q].y, c.y, sum[u]);
-                    sum[u] = fmaf(a[q].z, c.z, sum[u]); sum[u] = fmaf(a[q].w, c.w, sum[u]);
-                }
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            if (e0 + u > v.K) break;
-            float z = wave_sum(sum[u]);
-            if (n[u] >= 0 && v.bias) z += to_f(g.params[(int64_t)v.V * g.D + n[u]]);
-            if (lane == 0) g.zs[(int64_t)i * (v.K + 1) + e0 + u] = z;
-        }
-    }
+    for (int e0 = (threadIdx.x >> 6) * 4; e0 <= v.K; e0 += 16) named_logits(v, x, g.params, g.D, r, e0, g.zs + (int64_t)i * (v.K + 1));
 }
 
 // One workgroup per row of Xc.  Bound by reading the rows of W, scattered over all of it: 64 entries of 8192 rows of 1024, 1.07 GB,
@@ -346,14 +298,13 @@ __device__ __forceinline__ void teacher_loss(const VocabRows& v, int r, const fl
     *lse_tau = top * v.inv_tau + log_s;
 }
 
-// What a row's statistics come to, by a wavefront.
-__device__ __forceinline__ void row_losses(const VocabRows& v, int i, float top, float log0, float log1, const float* zs, const uint8_t* flags, int lane,
-                                           float* loss_ce, float* lse, float* loss_kd, float* lse_tau) {
-    const int r = v.list[i];
-    const float* z = zs + (int64_t)i * (v.K + 1);
-    const bool has = loss_ce && (!flags || flags[r] & HAS_LABEL);
+// What a row's statistics come to, by a wavefront; z: its named logits.
+__device__ __forceinline__ void row_losses(const VocabRows& v, int r, int flags, const float* z, float top, float log0, float log1, int lane,
+                                           const RowResults& out) {
+    float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
+    const bool has = loss_ce && (flags & HAS_LABEL);
     float kd = 0.f, l1 = 0.f;
-    if (loss_kd && (flags[r] & HAS_TEACHER)) teacher_loss(v, r, z, top, log1, lane, &kd, &l1);
+    if (loss_kd && (flags & HAS_TEACHER)) teacher_loss(v, r, z, top, log1, lane, &kd, &l1);
     if (lane == 0) {
         if (loss_ce) loss_ce[r] = has ? log0 + (top - z[0]) : 0.f;
         lse[r] = has ? top + log0 : 0.f;
@@ -361,16 +312,15 @@ __device__ __forceinline__ void row_losses(const VocabRows& v, int i, float top,
     }
 }
 
-// The statistics of a row joined, and its losses, a workgroup per row: for few rows.  stats: see FewRows and losses_kernel.
+// The statistics of a row joined, and its losses, a workgroup per row: for few rows, those that do not count among them.  stats: see
+// FewRows and losses_kernel.
 template <int N>
 __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const float* __restrict__ stats, int strips, int64_t stat_row, int64_t stat_kind,
-                                                         const float* __restrict__ zs, const uint8_t* __restrict__ flags, RowResults out) {
+                                                         const float* __restrict__ zs, RowResults out) {
     __shared__ float sh[3][4];
-    const int i = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    if (i >= v.plan->count) return;
-    float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
-    const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
-    const float* at = stats + i * stat_row;
+    const int r = blockIdx.x, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const float rate0 = N == 2 && !out.p[0] ? v.inv_tau : 1.f;
+    const float* at = stats + r * stat_row;
     float m = -INFINITY, s0 = 0.f, s1 = 0.f;
     for (int p0 = threadIdx.x; p0 < strips; p0 += 1024) {
         float a[4][N];
@@ -402,7 +352,7 @@ __global__ __launch_bounds__(256) void few_losses_kernel(VocabRows v, const floa
         t0 += sh[1][k] * expf((sh[0][k] - ref) * rate0);
         if (N == 3) t1 += sh[2][k] * expf((sh[0][k] - ref) * v.inv_tau);
     }
-    row_losses(v, i, top, logf(t0), logf(N == 3 ? t1 : t0), zs, flags, lane, loss_ce, lse, loss_kd, lse_tau);
+    row_losses(v, r, row_flags(v, r, lane), zs + (int64_t)r * (v.K + 1), top, logf(t0), logf(N == 3 ? t1 : t0), lane, out);
 }
 
 // The same for 16 rows per workgroup.  stats: [strips][N][Mp] = maximum m of a strip, sums of exp(z - m) and exp((z - m) / tau), the
@@ -417,9 +367,8 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
     __shared__ float sh[3][JOIN_ROWS][65];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, row = threadIdx.x & (JOIN_ROWS - 1), part = threadIdx.x / JOIN_ROWS;
     const int i0 = blockIdx.x * JOIN_ROWS, count = v.plan->count;
-    float *loss_ce = out.p[0], *lse = out.p[1], *loss_kd = out.p[2], *lse_tau = out.p[3];
     if (i0 >= count) return;
-    const float rate0 = N == 2 && !loss_ce ? v.inv_tau : 1.f;
+    const float rate0 = N == 2 && !out.p[0] ? v.inv_tau : 1.f;
     float m = -INFINITY, s0 = 0.f, s1 = 0.f;
     if (i0 + row < count) {
         const float* at = stats + i0 + row;
@@ -462,7 +411,8 @@ __global__ __launch_bounds__(1024) void losses_kernel(VocabRows v, const float* 
         }
         return;
     }
-    row_losses(v, i, top, logf(s0), logf(N == 3 ? s1 : s0), zs, flags, lane, loss_ce, lse, loss_kd, lse_tau);
+    const int r = v.list[i];
+    row_losses(v, r, flags ? flags[r] : HAS_LABEL, zs + (int64_t)i * (v.K + 1), top, logf(s0), logf(N == 3 ? s1 : s0), lane, out);
 }
 
 // ---------------------------------------------------------------------------------
@@ -552,11 +502,12 @@ static int vocab_check(const rev_vocab_cfg* c) {
 
 // Where the kernels of few rows (vocab_few.hip) take the place of the products in tiles; blocks: of 64 rows and 64 entries.  us, tiles / few
 // rows, D = 768 unless said.
-// Forward, bf16: 1 row, V = 50265: 35 / 27; 64: 35 / 32; 96: 35 / 43; V = 10007, 128 rows (314 blocks): 22 / 19; 256 (628): 22 / 25; V = 1000, 512:
-// 22 / 18.  float32: 128 rows, V = 50265: 182 / 120; V = 10007: 76 / 45; 256 rows, 10007: 77 / 73; 512, V = 1000, D = 384: 41 / 18.
+// Forward, bf16: 64 rows, V = 50265: 35 / 26; 96: 33 / 36; V = 10007, 128 rows (314 blocks): 21 / 15; 256 (628): 22 / 19; 640, V = 5000 (790): 22 /
+// 21; 300, V = 10007, D = 2048 (785): 35 / 38; 256, V = 15000 (940): 23 / 23; 1024, V = 5000, D = 256 (1264): 18 / 21.  float32: 128 rows, V = 50265: 182 /
+// 119; 256, V = 10007: 79 / 66; 640, V = 5000: 75 / 69; 1024, V = 4000 (1008): 74 / 77; 200, V = 20000 (1252): 94 / 102.
 static int64_t few_blocks(int64_t M, int64_t V) { return (M + 63) / 64 * ((V + 63) / 64); }
 static bool few_forward(const rev_vocab_cfg& c) {
-    return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 400;
+    return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 800;
 }
 // Backward.  bf16: V = 50265, 1 row: 87 / 76, 8: 87 / 81, 32: 81 / 106; V = 131072, D = 256, 4 rows: 97 / 70; V = 10007, 16 rows: 42 / 39, 32: 42 / 46;
 // V = 1000, 8: 26 / 22, 64: 27 / 30.  float32, whose tiles need W in parts first: V = 50265, 1 row: 359 / 118, 64: 378 / 259, 128: 395 / 491; V =
@@ -677,7 +628,7 @@ struct VocabRunner {
             LAUNCH((select_gather_kernel<T, P>), rows, block, v, g, at<uint8_t>(L.flags), at<int>(L.list), at<int>(L.place), zero, lim, at<VocabPlan>(L.plan));
             return REV_OK;
         }
-        if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v.labels, v.idx, v.logits, M, V, v.K, at<uint8_t>(L.flags));
+        if (v.idx) LAUNCH(row_flags_kernel, blocks_of(M, 4), dim3(256), v, at<uint8_t>(L.flags));
         LAUNCH(select_rows_kernel, dim3(SELECT_BLOCKS), dim3(1024), v.labels, flags(), M, V, at<int>(L.list), at<int>(L.place), zero, lim, at<VocabPlan>(L.plan));
         LAUNCH((gather_kernel<T, P>), rows, block, v, g, flags());
         return REV_OK;
@@ -687,8 +638,8 @@ struct VocabRunner {
         const int64_t kind = L.strips;
         const int strips = L.few_f || L.mid ? L.strips : (int)((std::min<int64_t>(L.span, V - (int64_t)piece * L.span) + 255) / 256 * 2);
         float* carry = at<float>(L.carry);
-        if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
-        else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), flags(), out);
+        if (L.few_f && dual()) LAUNCH(few_losses_kernel<3>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), out);
+        else if (L.few_f) LAUNCH(few_losses_kernel<2>, dim3(M), dim3(256), v, at<float>(L.stats), strips, 3 * kind, kind, at<float>(L.zs), out);
         else if (dual()) LAUNCH(losses_kernel<3>, blocks_of(M, JOIN_ROWS), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry,
                                 piece == 0, piece + 1 == pieces);
         else LAUNCH(losses_kernel<2>, blocks_of(M, JOIN_ROWS), dim3(1024), v, at<float>(L.stats), strips, L.Mp, at<float>(L.zs), flags(), out, carry, piece == 0,
@@ -705,7 +656,7 @@ struct VocabRunner {
         f.plan = v.plan; f.x = at<T>(L.xc); f.w = params; f.bias = bias(); f.stats = at<float>(L.stats); f.coef = at<float4>(L.coef);
         f.label = v.idx ? nullptr : at<int>(L.label); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
         f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
-        f.V = V; f.D = D; f.Dp = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = f.rows_out = M;
+        f.V = V; f.D = D; f.ldx = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = f.rows_out = M;
         f.range = L.range; f.ranges = L.ranges; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
         return f;
     }
@@ -773,8 +724,9 @@ struct VocabRunner {
             RC(prepare<kParts>(X, out, Cotangents{}));
             return forward_parts(out);
         }
-        RC(prepare<0>(X, out, Cotangents{}));
-        RC(few_logits<T>(s, few_args(), false, dual()));
+        FewRows<T> f = few_args();
+        f.plan = nullptr; f.x = (const T*)X; f.ldx = D; f.rows_x = M; f.named = v; f.zs = at<float>(L.zs);
+        RC(few_logits<T>(s, f, false, dual()));
         return join(out);
     }
     int backward(const void* X, const Cotangents& cot, void* dX, void* dparams) {
