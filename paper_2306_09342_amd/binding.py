@@ -440,50 +440,57 @@ def _vocab_new(shape, dtype, X, stream):
     return t
 
 
+def _vocab_want(t, dtype, shape, X):
+    _want(t, dtype, shape)
+    assert t.get_device() == X.get_device(), "tensors of different devices"
+
+
 def _vocab_common(cfg, params, X, workspace, stream, floats=(), ints=()):
     """Checks what the four calls have in common and returns the workspace.  floats, ints: (tensor or None, shape) of float32 and int32."""
-    _want(params, param_dtype(cfg), (rev_vocab_param_count(cfg),))
-    _want(X, param_dtype(cfg), (cfg.rows, cfg.d_model))
-    for dtype, group in ((torch.float32, floats), (torch.int32, ints)):
-        for t, shape in group:
-            if t is not None:
-                _want(t, dtype, shape)
-                assert t.device == X.device, "tensors of different devices"
-    assert params.device == X.device, "tensors of different devices"
+    rows, d, vocab, dtype = cfg.rows, cfg.d_model, cfg.vocab, param_dtype(cfg)
+    _want(X, dtype, (rows, d))
+    _vocab_want(params, dtype, (vocab * d + (vocab if cfg.bias else 0),), X)
+    for t, shape in floats:
+        if t is not None:
+            _vocab_want(t, torch.float32, shape, X)
+    for t, shape in ints:
+        if t is not None:
+            _vocab_want(t, torch.int32, shape, X)
     if workspace is None:
         return _vocab_new(rev_vocab_workspace_bytes(cfg), torch.uint8, X, stream)
-    _want(workspace, torch.uint8)
-    assert workspace.device == X.device, "tensors of different devices"
+    _vocab_want(workspace, torch.uint8, workspace.shape, X)
     return workspace
 
 
-def _vocab_call(name, X, stream, *args):
-    """The entry point on the device of X, which need not be the current one, and on its current stream unless another is given."""
-    handle = ctypes.c_void_p((torch.cuda.current_stream(X.device) if stream is None else stream).cuda_stream)
-    if X.device.index == torch.cuda.current_device():
-        _check(getattr(lib(), name)(*args, handle))
+def _vocab_call(name, cfg, X, stream, ws, *tensors):
+    """The entry point on the device of X, which need not be the current one, and on its current stream unless another is given.  For few
+    rows the host's part of a call is as long as the device's: nothing here that can be had for less."""
+    device = X.get_device()
+    handle = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    args = [None if t is None else t.data_ptr() for t in tensors]
+    if device == torch.cuda.current_device():
+        _check(getattr(lib(), name)(ctypes.byref(cfg), *args, ws.data_ptr(), ws.numel(), handle))
     else:
-        with torch.cuda.device(X.device):
-            _check(getattr(lib(), name)(*args, handle))
+        with torch.cuda.device(device):
+            _check(getattr(lib(), name)(ctypes.byref(cfg), *args, ws.data_ptr(), ws.numel(), handle))
 
 
 def _vocab_out(out, name, shape, dtype, X, stream):
-    t = (out or {}).get(name)
+    t = out.get(name) if out else None
     if t is None:
         return _vocab_new(shape, dtype, X, stream)
-    _want(t, dtype, shape)
-    assert t.device == X.device, "tensors of different devices"
+    _vocab_want(t, dtype, shape, X)
     return t
 
 
 def _vocab_grads(cfg, X, out, want, stream):
-    assert want and set(want) <= {"dX", "dparams"}, "want: dX, dparams or both"
+    assert want and all(w in ("dX", "dparams") for w in want), "want: dX, dparams or both"
     res = {}
     if "dX" in want:
         res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X, stream)
     if "dparams" in want:
         dtype = torch.bfloat16 if cfg.grad_mode == REV_MODE_BF16 else torch.float32
-        res["dparams"] = _vocab_out(out, "dparams", (rev_vocab_param_count(cfg),), dtype, X, stream)
+        res["dparams"] = _vocab_out(out, "dparams", (cfg.vocab * cfg.d_model + (cfg.vocab if cfg.bias else 0),), dtype, X, stream)
     return res
 
 
@@ -491,8 +498,7 @@ def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=No
     """Softmax cross entropy of the rows of X over the vocabulary: {"loss", "lse"}, float32 [rows]; labels int32 [rows]."""
     ws = _vocab_common(cfg, params, X, workspace, stream, ints=[(labels, (cfg.rows,))])
     loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X, stream) for n in ("loss", "lse"))
-    _vocab_call("rev_xent_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(loss), _ptr(lse), _ptr(ws),
-                ws.numel())
+    _vocab_call("rev_xent_forward", cfg, X, stream, ws, params, X, labels, loss, lse)
     return {"loss": loss, "lse": lse}
 
 
@@ -500,8 +506,7 @@ def rev_xent_backward(cfg, params, X, labels, lse, dloss, workspace=None, stream
     """Gradients of sum(dloss * loss), with the lse of the forward call: the members of `want`."""
     ws = _vocab_common(cfg, params, X, workspace, stream, [(lse, (cfg.rows,)), (dloss, (cfg.rows,))], ints=[(labels, (cfg.rows,))])
     res = _vocab_grads(cfg, X, out, want, stream)
-    _vocab_call("rev_xent_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(lse), _ptr(dloss),
-                _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws), ws.numel())
+    _vocab_call("rev_xent_backward", cfg, X, stream, ws, params, X, labels, lse, dloss, res.get("dX"), res.get("dparams"))
     return res
 
 
@@ -514,8 +519,8 @@ def rev_distill_forward(cfg, params, X, teacher_idx, teacher_logits, labels=None
            "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X, stream)}
     if labels is not None:
         res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X, stream)
-    _vocab_call("rev_distill_forward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
-                _ptr(teacher_logits), _ptr(res.get("loss_ce")), _ptr(res["loss"]), _ptr(res["lse"]), _ptr(ws), ws.numel())
+    _vocab_call("rev_distill_forward", cfg, X, stream, ws, params, X, labels, teacher_idx, teacher_logits, res.get("loss_ce"), res["loss"],
+                res["lse"])
     return res
 
 
@@ -526,9 +531,8 @@ def rev_distill_backward(cfg, params, X, teacher_idx, teacher_logits, lse, dloss
     ws = _vocab_common(cfg, params, X, workspace, stream, [(teacher_logits, top), (lse, (2, cfg.rows)), (dloss, row), (dloss_ce, row)],
                        ints=[(labels, row), (teacher_idx, top)])
     res = _vocab_grads(cfg, X, out, want, stream)
-    _vocab_call("rev_distill_backward", X, stream, ctypes.byref(cfg), _ptr(params), _ptr(X), _ptr(labels), _ptr(teacher_idx),
-                _ptr(teacher_logits), _ptr(lse), _ptr(dloss_ce), _ptr(dloss), _ptr(res.get("dX")), _ptr(res.get("dparams")), _ptr(ws),
-                ws.numel())
+    _vocab_call("rev_distill_backward", cfg, X, stream, ws, params, X, labels, teacher_idx, teacher_logits, lse, dloss_ce, dloss,
+                res.get("dX"), res.get("dparams"))
     return res
 
 

@@ -191,13 +191,19 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 // What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
 // entries, float32: one row 58 us (5.3 TB/s of W and dW), 32 rows 102 us.
 template <typename T, typename TG, int MB>
-__global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db) {
+__global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
     extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1]
     const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int count = __builtin_amdgcn_readfirstlane(p.plan->count);
-    const int r = blockIdx.x / p.col_groups, cg = blockIdx.x - r * p.col_groups, P = p.range + 1;
+    int block = blockIdx.x;
+    if (apart) {                                                   // dW in the first half of the workgroups, dx in the second
+        const int half = gridDim.x >> 1;
+        if (block < half) want_dx = 0;
+        else { block -= half; dparams = nullptr; }
+    }
+    const int r = block / p.col_groups, cg = block - r * p.col_groups, P = p.range + 1;
     const int v0 = r * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
     // chunks of 32 entries of a row, two per wavefront, eight of each in flight
     const int per = p.range >> 5, chunks = rows32 * per;
@@ -236,7 +242,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
         const T* x = p.x + dc;
         const T* w = p.w + (int64_t)v0 * p.D + dc;
         // up to 32 rows of x stay in registers
-        constexpr int KEPT = MB == 1 ? 16 : 1;
+        constexpr int KEPT = MB == 1 ? 16 : 1, XS = 16;
         unsigned kept[KEPT];
         if (MB == 1 && dparams) {
 #pragma unroll
@@ -258,18 +264,18 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
                 for (int s = 0; s < KEPT; ++s)
                     if (2 * s < count) add(s, kept[s]);
             } else {
-                unsigned xv[8], next[8];
-                auto load = [&](unsigned (&to)[8], int s0) {
+                unsigned xv[XS], next[XS];
+                auto load = [&](unsigned (&to)[XS], int s0) {
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx);
+                    for (int s = 0; s < XS; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx);
                 };
                 load(next, 0);
-                for (int s0 = 0; 2 * s0 < count; s0 += 8) {
+                for (int s0 = 0; 2 * s0 < count; s0 += XS) {       // (32 rows at a time, as many as there are of dz)
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) xv[s] = next[s];
-                    load(next, s0 + 8);
+                    for (int s = 0; s < XS; ++s) xv[s] = next[s];
+                    load(next, s0 + XS);
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) add(s0 + s, xv[s]);
+                    for (int s = 0; s < XS; ++s) add(s0 + s, xv[s]);
                 }
             }
             if (d < p.D) {
@@ -289,22 +295,22 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
                 }
             }
         }
+        unsigned wv[16], next[16];                                 // 32 entries, asked for 32 ahead
+        auto load = [&](unsigned (&to)[16], int vb) {
+#pragma unroll
+            for (int s = 0; s < 16; ++s) to[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
+        };
+        if (want_dx) load(next, 0);
         for (int m0 = 0; m0 < rows32 && want_dx; m0 += 32 * MB) {
             f32x16_t acc[MB][CS];
 #pragma unroll
             for (int m = 0; m < MB; ++m)
 #pragma unroll
                 for (int q = 0; q < CS; ++q) clear(acc[m][q]);
-            unsigned wv[16], next[16];                             // 32 entries, asked for 32 ahead
-            auto load = [&](unsigned (&to)[16], int vb) {
-#pragma unroll
-                for (int s = 0; s < 16; ++s) to[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
-            };
-            load(next, 0);
             for (int vb = 0; vb < nv; vb += 32) {
 #pragma unroll
                 for (int s = 0; s < 16; ++s) wv[s] = next[s];
-                load(next, vb + 32);
+                load(next, vb + 32 < nv ? vb + 32 : 0);
 #pragma unroll
                 for (int s = 0; s < 16; ++s) {
                     float f[CS];
@@ -404,11 +410,15 @@ template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, boo
 template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, void* dparams, bool grad_bf16, bool db) {
     ProfScope ps(K_VOCAB, s, 2.0 * p.rows * p.V * p.D * (want_dx + (dparams != nullptr)));
     const int rows32 = (p.rows + 31) / 32 * 32, lds = rows32 * (p.range + 1) * 4;
-    const dim3 grid((unsigned)(p.ranges * p.col_groups)), block(256);
+    // Few workgroups wait for memory most of the time: dW and dx in workgroups of their own.  Gradients in us, together / apart: float32, 128 rows,
+    // D = 384, V = 1000 (96 workgroups): 34 / 29; 512, 768, 1000 (192): 80 / 71; 333, 200, 5003 (314): 88 / 85; 64, 768, 10007 (939): 80 / 82;
+    // bf16, 8, 768, 10007 (939): 35 / 37.
+    const int blocks = p.ranges * p.col_groups, apart = want_dx && dparams && blocks <= 384;
+    const dim3 grid((unsigned)(blocks << apart)), block(256);
 #define GRADS(TG, MB) do {                                                                                             \
         static LdsLimit lim;                                                                                           \
         if (int rc = lim.ensure(reinterpret_cast<const void*>(few_grads_kernel<T, TG, MB>), 160 * 1024)) return rc;    \
-        hipLaunchKernelGGL((few_grads_kernel<T, TG, MB>), grid, block, lds, s, p, (int)want_dx, (TG*)dparams, (int)db); \
+        hipLaunchKernelGGL((few_grads_kernel<T, TG, MB>), grid, block, lds, s, p, (int)want_dx, (TG*)dparams, (int)db, apart); \
         REV_HIP(hipGetLastError());                                                                                    \
         return REV_OK;                                                                                                 \
     } while (0)
