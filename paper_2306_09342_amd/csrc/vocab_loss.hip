@@ -509,13 +509,15 @@ static int64_t few_blocks(int64_t M, int64_t V) { return (M + 63) / 64 * ((V + 6
 static bool few_forward(const rev_vocab_cfg& c) {
     return c.rows <= (c.mode == REV_MODE_BF16 ? 64 : 128) || few_blocks(c.rows, c.vocab) <= 800;
 }
-// Backward.  bf16: V = 50265, 1 row: 87 / 76, 8: 87 / 81, 32: 81 / 106; V = 131072, D = 256, 4 rows: 97 / 70; V = 10007, 16 rows: 42 / 39, 32: 42 / 46;
-// V = 1000, 8: 26 / 22, 64: 27 / 30.  float32, whose tiles need W in parts first: V = 50265, 1 row: 359 / 118, 64: 378 / 259, 128: 395 / 491; V =
-// 10007, 128: 151 / 137; V = 1000, 512 (128 blocks): 127 / 87; V = 5003, D = 200, 333 (474): 101 / 91; D = 768, 256 (316): 132 / 140; D = 256, 500 (632):
-// 101 / 123; V = 20000, D = 384, 200 (1252): 175 / 192.
+// Backward, where their time goes with the number of products (rows x D x V, in millions) and the tiles' does not.  bf16: 1 row, V = 50265 (39): 81 /
+// 76; 64, V = 1000 (49): 28 / 25; 16, V = 10007 (123): 43 / 37; 64, V = 5000, D = 512 (164): 43 / 36; 64, V = 4000 (197): 39 / 37; 48, V = 6000 (221): 35 /
+// 46; 8, V = 50265 (309): 81 / 80; 8, V = 50265, D = 1024 (412): 91 / 115; more than 64 rows: 128, V = 1000 (98): 28 / 33.  float32, whose tiles need W in
+// parts first: 16, V = 1000 (12): 89 / 25; 64, V = 50265 (2470): 362 / 247; 64, V = 32000, D = 2048 (4194): 568 / 379; 128, V = 10007, D = 384 (492): 95 /
+// 80; 640, V = 1000 (492): 137 / 110; 100, V = 10007, D = 512 (512): 103 / 106; 500, V = 5000, D = 256 (640): 108 / 116; 128, V = 10007 (984): 125 / 133.
 static bool few_backward(const rev_vocab_cfg& c) {
-    if (c.mode == REV_MODE_BF16) return c.rows <= 8 || (c.rows <= 16 && c.vocab <= 16384);
-    return c.rows <= 64 || (c.rows <= 128 && c.vocab <= 16384) || (c.rows <= 512 && few_blocks(c.rows, c.vocab) <= 480);
+    const int64_t products = (int64_t)c.rows * c.d_model * c.vocab;
+    if (c.mode == REV_MODE_BF16) return c.rows <= 64 && products <= 170000000;
+    return c.rows <= 64 || (c.rows <= 768 && products <= 500000000);
 }
 // dz alone by them, the gradients in tiles (bf16).  V = 1000, 128 rows: 35 / 29, 512: 45 / 39; V = 10007, 128 rows: 54 / 53.
 static bool few_for_dz(const rev_vocab_cfg& c) { return c.mode == REV_MODE_BF16 && !few_backward(c) && few_blocks(c.rows, c.vocab) <= 160; }
