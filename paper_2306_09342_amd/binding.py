@@ -431,10 +431,10 @@ def rev_vocab_workspace_bytes(cfg: RevVocabCfg) -> int:
     return _check(lib().rev_vocab_workspace_bytes(ctypes.byref(cfg)))
 
 
-def _vocab_new(shape, dtype, X, stream):
+def _vocab_new(shape, dtype, X, stream, like=None):
     """A tensor on the device of X for a call on `stream`: allocated for the current stream, so kept from being used again there before the
-    call's work is done if that is on another one."""
-    t = torch.empty(shape, dtype=dtype, device=X.device)
+    call's work is done if that is on another one.  `like`: one of the same shape, type and device (the quicker way)."""
+    t = X.new_empty(shape, dtype=dtype) if like is None else torch.empty_like(like)
     if stream is not None:
         t.record_stream(stream)
     return t
@@ -475,10 +475,10 @@ def _vocab_call(name, cfg, X, stream, ws, *tensors):
             _check(getattr(lib(), name)(ctypes.byref(cfg), *args, ws.data_ptr(), ws.numel(), handle))
 
 
-def _vocab_out(out, name, shape, dtype, X, stream):
+def _vocab_out(out, name, shape, dtype, X, stream, like=None):
     t = out.get(name) if out else None
     if t is None:
-        return _vocab_new(shape, dtype, X, stream)
+        return _vocab_new(shape, dtype, X, stream, like)
     _vocab_want(t, dtype, shape, X)
     return t
 
@@ -487,7 +487,7 @@ def _vocab_grads(cfg, X, out, want, stream):
     assert want and all(w in ("dX", "dparams") for w in want), "want: dX, dparams or both"
     res = {}
     if "dX" in want:
-        res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X, stream)
+        res["dX"] = _vocab_out(out, "dX", (cfg.rows, cfg.d_model), param_dtype(cfg), X, stream, like=X)
     if "dparams" in want:
         dtype = torch.bfloat16 if cfg.grad_mode == REV_MODE_BF16 else torch.float32
         res["dparams"] = _vocab_out(out, "dparams", (cfg.vocab * cfg.d_model + (cfg.vocab if cfg.bias else 0),), dtype, X, stream)
@@ -497,7 +497,8 @@ def _vocab_grads(cfg, X, out, want, stream):
 def rev_xent_forward(cfg, params, X, labels, workspace=None, stream=None, out=None):
     """Softmax cross entropy of the rows of X over the vocabulary: {"loss", "lse"}, float32 [rows]; labels int32 [rows]."""
     ws = _vocab_common(cfg, params, X, workspace, stream, ints=[(labels, (cfg.rows,))])
-    loss, lse = (_vocab_out(out, n, (cfg.rows,), torch.float32, X, stream) for n in ("loss", "lse"))
+    loss = _vocab_out(out, "loss", (cfg.rows,), torch.float32, X, stream)
+    lse = _vocab_out(out, "lse", (cfg.rows,), torch.float32, X, stream, like=loss)
     _vocab_call("rev_xent_forward", cfg, X, stream, ws, params, X, labels, loss, lse)
     return {"loss": loss, "lse": lse}
 
@@ -518,7 +519,7 @@ def rev_distill_forward(cfg, params, X, teacher_idx, teacher_logits, labels=None
     res = {"loss": _vocab_out(out, "loss", (cfg.rows,), torch.float32, X, stream),
            "lse": _vocab_out(out, "lse", (2, cfg.rows), torch.float32, X, stream)}
     if labels is not None:
-        res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X, stream)
+        res["loss_ce"] = _vocab_out(out, "loss_ce", (cfg.rows,), torch.float32, X, stream, like=res["loss"])
     _vocab_call("rev_distill_forward", cfg, X, stream, ws, params, X, labels, teacher_idx, teacher_logits, res.get("loss_ce"), res["loss"],
                 res["lse"])
     return res
