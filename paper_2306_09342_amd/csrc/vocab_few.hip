@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 // What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
 // entries, float32: one row 58 us (5.3 TB/s of W and dW), 32 rows 102 us.
 template <typename T, typename TG, int MB>
-__global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
+__global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
     extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1]
     const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
@@ -232,21 +232,21 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
         if constexpr (CS == 1) f[0] = __uint_as_float(u);
         else { f[0] = __uint_as_float(u << 16); f[1] = __uint_as_float(u & 0xFFFF0000u); }
     };
-    auto word = [&](const T* at) { return *reinterpret_cast<const unsigned*>(at); };
+    // (32-bit offsets from where the workgroup's rows begin: less than 1024 rows of x, 256 of W)
+    auto word = [&](const T* at, unsigned offset) { return *reinterpret_cast<const unsigned*>(reinterpret_cast<const char*>(at) + offset); };
     auto clear = [&](f32x16_t& c) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) c[v] = 0.f;
     };
     for (int b = cg * 4 + wave; b < blocks; b += 4 * p.col_groups) {
         const int d = b * COLS + CS * fr, dc = min(d, p.D - CS);   // columns beyond D read the last ones again (never stored)
-        const T* x = p.x + dc;
-        const T* w = p.w + (int64_t)v0 * p.D + dc;
+        const T* w = p.w + (int64_t)v0 * p.D;
         // up to 32 rows of x stay in registers
         constexpr int KEPT = MB == 1 ? 16 : 1, XS = 16;
         unsigned kept[KEPT];
         if (MB == 1 && dparams) {
 #pragma unroll
-            for (int s = 0; s < KEPT; ++s) kept[s] = 2 * s < count ? word(x + (int64_t)(2 * s + g) * p.ldx) : 0u;
+            for (int s = 0; s < KEPT; ++s) kept[s] = 2 * s < count ? word(p.x, (unsigned)((2 * s + g) * p.ldx + dc) * sizeof(T)) : 0u;
         }
         for (int vb = 0; vb < nv && dparams; vb += 32) {
             f32x16_t acc[CS];
@@ -267,7 +267,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
                 unsigned xv[XS], next[XS];
                 auto load = [&](unsigned (&to)[XS], int s0) {
 #pragma unroll
-                    for (int s = 0; s < XS; ++s) to[s] = word(x + (int64_t)min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx);
+                    for (int s = 0; s < XS; ++s) to[s] = word(p.x, (unsigned)(min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx + dc) * sizeof(T));
                 };
                 load(next, 0);
                 for (int s0 = 0; 2 * s0 < count; s0 += XS) {       // (32 rows at a time, as many as there are of dz)
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(256, 2) void few_grads_kernel(FewRows<T> p, int wan
         unsigned wv[16], next[16];                                 // 32 entries, asked for 32 ahead
         auto load = [&](unsigned (&to)[16], int vb) {
 #pragma unroll
-            for (int s = 0; s < 16; ++s) to[s] = word(w + (int64_t)min(vb + 2 * s + g, nv - 1) * p.D);
+            for (int s = 0; s < 16; ++s) to[s] = word(w, (unsigned)(min(vb + 2 * s + g, nv - 1) * p.D + dc) * sizeof(T));
         };
         if (want_dx) load(next, 0);
         for (int m0 = 0; m0 < rows32 && want_dx; m0 += 32 * MB) {
