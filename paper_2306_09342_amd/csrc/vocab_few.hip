@@ -191,9 +191,9 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 // What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
 // entries, float32: one row 58 us (5.3 TB/s of W and dW), 32 rows 102 us.
 template <typename T, typename TG, int MB>
-__global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
-    extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1]
+    extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1], 256 more for db
     const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int count = __builtin_amdgcn_readfirstlane(p.plan->count);
@@ -205,34 +205,48 @@ __global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int wan
     }
     const int r = block / p.col_groups, cg = block - r * p.col_groups, P = p.range + 1;
     const int v0 = r * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
-    // chunks of 32 entries of a row, two per wavefront, eight of each in flight
-    const int per = p.range >> 5, chunks = rows32 * per;
-    for (int k0 = wave * 2 + g; k0 < chunks; k0 += 64) {
-        float u[8];
+    // four entries of a row per thread and load, eight of these in flight (dz has whole quads, zeros behind the vocabulary)
+    const int per = p.range >> 2, quads = rows32 * per;
+    for (int k0 = threadIdx.x; k0 < quads; k0 += 2048) {
+        f32x4_t u[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const int k = k0 + 8 * q, i = k / per, c = (k - i * per) * 32 + fr;
-            u[q] = i < count && c < nv ? p.dz[i * p.ldz + v0 + c] : 0.f;
+            const int k = k0 + 256 * q, i = k / per, c = (k - i * per) * 4;
+            u[q] = i < count && v0 + c < p.ldz ? *reinterpret_cast<const f32x4_t*>(p.dz + i * p.ldz + v0 + c) : f32x4_t{0.f, 0.f, 0.f, 0.f};
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const int k = k0 + 8 * q, i = k / per, c = (k - i * per) * 32 + fr;
-            if (k < chunks) dzs[i * P + c] = u[q];
+            const int k = k0 + 256 * q, i = k / per, c = (k - i * per) * 4;
+            if (k < quads) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) dzs[i * P + c + e] = u[q][e];
+            }
         }
     }
     __syncthreads();
-    if (db && dparams && cg == 0)
-        for (int c = threadIdx.x; c < nv; c += 256) {
+    if (db && dparams && cg == 0) {                                // every eighth row per 32 threads, 32 entries at a time
+        float (*sums)[32] = reinterpret_cast<float (*)[32]>(dzs + rows32 * P);
+        const int c = threadIdx.x & 31, part = threadIdx.x >> 5;
+        for (int vb = 0; vb < nv; vb += 32) {
             float s = 0.f;
-            for (int i = 0; i < count; ++i) s += dzs[i * P + c];
-            dparams[(int64_t)p.V * p.D + v0 + c] = from_f<TG>(s);
+#pragma unroll 4
+            for (int i = part; i < rows32; i += 8) s += dzs[i * P + vb + c];
+            sums[part][c] = s;
+            __syncthreads();
+            if (part == 0 && vb + c < nv) {
+#pragma unroll
+                for (int k = 1; k < 8; ++k) s += sums[k][c];
+                dparams[(int64_t)p.V * p.D + v0 + vb + c] = from_f<TG>(s);
+            }
+            __syncthreads();
         }
+    }
     const int blocks = (p.D + COLS - 1) / COLS;
     auto columns = [&](unsigned u, float (&f)[CS]) {
         if constexpr (CS == 1) f[0] = __uint_as_float(u);
         else { f[0] = __uint_as_float(u << 16); f[1] = __uint_as_float(u & 0xFFFF0000u); }
     };
-    // (32-bit offsets from where the workgroup's rows begin: less than 1024 rows of x, 256 of W)
+    // (what differs between the lanes in 32 bits)
     auto word = [&](const T* at, unsigned offset) { return *reinterpret_cast<const unsigned*>(reinterpret_cast<const char*>(at) + offset); };
     auto clear = [&](f32x16_t& c) {
 #pragma unroll
@@ -242,7 +256,7 @@ __global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int wan
         const int d = b * COLS + CS * fr, dc = min(d, p.D - CS);   // columns beyond D read the last ones again (never stored)
         const T* w = p.w + (int64_t)v0 * p.D;
         // up to 32 rows of x stay in registers
-        constexpr int KEPT = MB == 1 ? 16 : 1, XS = 16;
+        constexpr int KEPT = MB == 1 ? 16 : 1;
         unsigned kept[KEPT];
         if (MB == 1 && dparams) {
 #pragma unroll
@@ -252,30 +266,45 @@ __global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int wan
             f32x16_t acc[CS];
 #pragma unroll
             for (int q = 0; q < CS; ++q) clear(acc[q]);
-            auto add = [&](int s, unsigned u) {
-                const float a = dzs[(2 * s + g) * P + vb + fr];    // (rows up to whole 32 are there)
-                float f[CS];
-                columns(u, f);
-#pragma unroll
-                for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
-            };
             if constexpr (MB == 1) {
+                auto add = [&](int s, unsigned u) {
+                    const float a = dzs[(2 * s + g) * P + vb + fr];    // (rows up to whole 32 are there)
+                    float f[CS];
+                    columns(u, f);
+#pragma unroll
+                    for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
+                };
 #pragma unroll
                 for (int s = 0; s < KEPT; ++s)
                     if (2 * s < count) add(s, kept[s]);
             } else {
-                unsigned xv[XS], next[XS];
-                auto load = [&](unsigned (&to)[XS], int s0) {
+                // 32 rows at a time, as many as there are of dz; the next ones asked for first
+                unsigned even[16], odd[16];
+                auto load = [&](unsigned (&to)[16], int i0) {
+                    const T* at = p.x + (int64_t)min(i0, p.rows_x - 32) * p.ldx;
 #pragma unroll
-                    for (int s = 0; s < XS; ++s) to[s] = word(p.x, (unsigned)(min(2 * (s0 + s) + g, p.rows_x - 1) * p.ldx + dc) * sizeof(T));
+                    for (int s = 0; s < 16; ++s) to[s] = word(at + 2 * s * p.ldx, (unsigned)(g * p.ldx + dc) * sizeof(T));
+                    __builtin_amdgcn_sched_barrier(0);             // (the compiler moves them behind the products)
                 };
-                load(next, 0);
-                for (int s0 = 0; 2 * s0 < count; s0 += XS) {       // (32 rows at a time, as many as there are of dz)
+                auto add = [&](unsigned (&u)[16], int i0) {
+                    int at = (i0 + g) * P + vb + fr;
+                    asm volatile("" : "+v"(at));                   // (no sixteen addresses kept over the loop)
 #pragma unroll
-                    for (int s = 0; s < XS; ++s) xv[s] = next[s];
-                    load(next, s0 + XS);
+                    for (int s = 0; s < 16; ++s) {
+                        const float a = dzs[at + 2 * s * P];
+                        float f[CS];
+                        columns(u[s], f);
 #pragma unroll
-                    for (int s = 0; s < XS; ++s) add(s0 + s, xv[s]);
+                        for (int q = 0; q < CS; ++q) acc[q] = mfma_f32(a, f[q], acc[q]);
+                    }
+                };
+                load(even, 0);
+                for (int i0 = 0; i0 < count; i0 += 64) {
+                    load(odd, i0 + 32);
+                    add(even, i0);
+                    if (i0 + 32 >= count) break;
+                    load(even, i0 + 64);
+                    add(odd, i0 + 32);
                 }
             }
             if (d < p.D) {
@@ -295,38 +324,45 @@ __global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int wan
                 }
             }
         }
-        unsigned wv[16], next[16];                                 // 32 entries, asked for 32 ahead
-        auto load = [&](unsigned (&to)[16], int vb) {
+        if (!want_dx || rows32 == 0) continue;
+        constexpr int DB = CS == 2 ? 1 : MB;                       // blocks of 32 rows at a time
+        unsigned even[16], odd[16];                                // 32 entries; the next 32, of the range or for the next rows, asked for first
+        f32x16_t acc[DB][CS];
+        int m0 = 0, vb = 0;
+        const unsigned both = (unsigned)(g * p.D + dc) * (unsigned)sizeof(T);
+        auto load = [&](unsigned (&to)[16], int v) {
 #pragma unroll
-            for (int s = 0; s < 16; ++s) to[s] = word(w, (unsigned)(min(vb + 2 * s + g, nv - 1) * p.D + dc) * sizeof(T));
+            for (int s = 0; s < 16; ++s)                           // rows beyond the range, where dz is 0, read its last one again
+                to[s] = word(w + (int64_t)min(v + 2 * s, nv - 1) * p.D, v + 2 * s + 1 < nv ? both : (unsigned)dc * (unsigned)sizeof(T));
+            __builtin_amdgcn_sched_barrier(0);
         };
-        if (want_dx) load(next, 0);
-        for (int m0 = 0; m0 < rows32 && want_dx; m0 += 32 * MB) {
-            f32x16_t acc[MB][CS];
+        auto step = [&](unsigned (&u)[16], unsigned (&next)[16]) {
+            load(next, vb + 32 < nv ? vb + 32 : 0);
+            if (vb == 0) {
 #pragma unroll
-            for (int m = 0; m < MB; ++m)
+                for (int m = 0; m < DB; ++m)
 #pragma unroll
-                for (int q = 0; q < CS; ++q) clear(acc[m][q]);
-            for (int vb = 0; vb < nv; vb += 32) {
+                    for (int q = 0; q < CS; ++q) clear(acc[m][q]);
+            }
+            const float* a[DB];                                    // blocks beyond the last repeat it (not stored)
 #pragma unroll
-                for (int s = 0; s < 16; ++s) wv[s] = next[s];
-                load(next, vb + 32 < nv ? vb + 32 : 0);
+            for (int m = 0; m < DB; ++m) a[m] = dzs + (min(m0 + m * 32, rows32 - 32) + fr) * P + vb + g;
 #pragma unroll
-                for (int s = 0; s < 16; ++s) {
-                    float f[CS];
-                    columns(wv[s], f);
+            for (int s = 0; s < 16; ++s) {
+                float f[CS];
+                columns(u[s], f);
 #pragma unroll
-                    for (int m = 0; m < MB; ++m) {
-                        const int i = min(m0 + m * 32, rows32 - 32) + fr;    // blocks beyond the last repeat it (not stored)
-                        const float a = dzs[i * P + vb + 2 * s + g];
+                for (int m = 0; m < DB; ++m) {
+                    const float z = a[m][2 * s];
 #pragma unroll
-                        for (int q = 0; q < CS; ++q) acc[m][q] = mfma_f32(a, f[q], acc[m][q]);
-                    }
+                    for (int q = 0; q < CS; ++q) acc[m][q] = mfma_f32(z, f[q], acc[m][q]);
                 }
             }
+            vb += 32;
+            if (vb < nv) return;
             if (d < p.D) {
 #pragma unroll
-                for (int m = 0; m < MB; ++m)
+                for (int m = 0; m < DB; ++m)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const int i = m0 + m * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
@@ -336,6 +372,15 @@ __global__ __launch_bounds__(256, 3) void few_grads_kernel(FewRows<T> p, int wan
                         else *reinterpret_cast<float2*>(out) = make_float2(acc[m][0][v], acc[m][1][v]);
                     }
             }
+            vb = 0;
+            m0 += 32 * DB;
+        };
+        load(even, 0);
+        for (;;) {
+            step(even, odd);
+            if (m0 >= rows32) break;
+            step(odd, even);
+            if (m0 >= rows32) break;
         }
     }
 }
@@ -373,11 +418,12 @@ __global__ __launch_bounds__(256) void few_dx_rows_kernel(FewRows<T> p, const in
 }
 
 // Ranges of the vocabulary and groups of columns: about 320 ranges, of at most 256 entries (of fewer where their dz would not leave LDS
-// for two workgroups), each by as many workgroups as it has groups of four column blocks.  32 rows of 768 to 50265 entries, loss and gradients
-// backward in us by entries per range and groups, bf16 / float32: 224, 2: 126 / 149; 224, 3: 121 / 143; 128, 3: 118 / 157; 64, 3: 129 / 178.
+// for two workgroups) and, from 5120 entries on, of no fewer than 64, each by as many workgroups as it has groups of four column blocks.  32 rows
+// of 768 to 50265 entries, loss and gradients backward in us by entries per range and groups, bf16 / float32: 224, 2: 126 / 149; 224, 3: 121 / 143; 128,
+// 3: 118 / 157; 64, 3: 129 / 178.  10007 entries in ranges of 32 / 64: 16 bf16 rows of 768 36 / 32, 128 float32 rows of 384 77 / 69.
 void few_ranges(int rows, int V, int D, int es, int* range, int* ranges, int* col_groups) {
     const int blocks32 = (V + 31) / 32, rows32 = (rows + 31) / 32 * 32;
-    int per = (blocks32 + 319) / 320;
+    int per = blocks32 > 160 ? std::max(2, (blocks32 + 319) / 320) : 1;
     while (per > 1 && (per > 8 || rows32 * (per * 32 + 1) * 4 > 72 * 1024)) --per;
     *range = per * 32;
     *ranges = (blocks32 + per - 1) / per;
@@ -409,7 +455,7 @@ template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, boo
 }
 template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, void* dparams, bool grad_bf16, bool db) {
     ProfScope ps(K_VOCAB, s, 2.0 * p.rows * p.V * p.D * (want_dx + (dparams != nullptr)));
-    const int rows32 = (p.rows + 31) / 32 * 32, lds = rows32 * (p.range + 1) * 4;
+    const int rows32 = (p.rows + 31) / 32 * 32, lds = rows32 * (p.range + 1) * 4 + 1024;
     // Few workgroups wait for memory most of the time: dW and dx in workgroups of their own.  Gradients in us, together / apart: float32, 128 rows,
     // D = 384, V = 1000 (96 workgroups): 34 / 29; 512, 768, 1000 (192): 80 / 71; 333, 200, 5003 (314): 88 / 85; 64, 768, 10007 (939): 80 / 82;
     // bf16, 8, 768, 10007 (939): 35 / 37.
