@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 // the two products of a pair one after the other).
 //
 // What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
-// entries, float32: one row 58 us (5.3 TB/s of W and dW), 32 rows 102 us.
+// entries, float32: one row 67 us (4.6 TB/s of W and dW), 32 rows 87 us.
 template <typename T, typename TG, int MB>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
