@@ -108,6 +108,9 @@ struct VocabGemm {
     int piece, span;                // piece: its number; span: its width in the forward pass, a multiple of 256
     int losses;                     // whose exponentials without `dual`: LOSS_CE, LOSS_KD or both (tau = 1)
     float inv_tau;
+    float* dw_parts;                // dW and db of a range of rows, where the rows are cut into several: as dparams, dw_stride floats each
+    int64_t dw_stride;
+    int dw_splits;
     double work;                    // of a product over a piece, for the timing of kernel families
 };
 // x = p[0] + p[1] + p[2] to 2^-25 of |x|; an infinity (also of a value beyond the largest bf16, 3.39e38) or NaN is p[0] alone.
@@ -122,6 +125,7 @@ __device__ __forceinline__ void split3(float x, bf16 (&p)[3]) {
 // mid: tiles of 128 instead of 256; blocks: most of the latter
 template <typename T> int vocab_logits(hipStream_t s, const VocabGemm& p, bool grad, bool dual, bool mid, int64_t blocks);
 template <typename T> int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw_blocks, void* dparams, bool grad_bf16, bool db);
+int vocab_dw_sum(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, int64_t n);
 template <typename T> int vocab_dx_rows(hipStream_t s, const VocabGemm& p, const int* list, const int* place, int M, T* dX);
 
 // Few rows (vocab_few.hip): the statistics of the logits of all rows and the logits that they name; or dz of the whole vocabulary in

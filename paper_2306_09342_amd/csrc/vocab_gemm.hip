@@ -3,7 +3,7 @@
 //              forward    a row's maximum and sum of exponentials over half a tile's entries leave the kernel,
 //              backward   dz of a piece of the vocabulary does, in bf16;
 //   dx       dx[i, d] = sum over v of dz[i, v] W[v, d], the vocabulary cut into ranges where there are few tiles;
-//   dw       dW[v, d] = sum over i of dz[i, v] x[i, d].
+//   dw       dW[v, d] = sum over i of dz[i, v] x[i, d], the rows cut into ranges where there are few tiles.
 //
 // One workgroup of 8 wavefronts per CU, 128 x 64 of the tile per wavefront.  A stage is 64 of the contraction; it travels as four
 // parts of 16 KB (two halves of each operand) through two stages of LDS.  A part is requested again, for the stage after
@@ -732,8 +732,9 @@ __global__ __launch_bounds__(256) void vocab_dx_rows_kernel(VocabGemm p, const i
         }
 }
 
-// dW of 256 entries of a piece and 256 columns over all rows, and, in the workgroups behind the tiles, db of 256 entries each: these
-// find the CUs that the last round of tiles leaves idle.
+// dW of 256 entries of a piece and 256 columns over a range of the rows, all of them unless there are few tiles, and, in the workgroups
+// behind the tiles, db of 256 entries each: these find the CUs that the last round of tiles leaves idle.  The sums of several ranges go to
+// places of their own, in float32 (vocab_dw_sum_kernel).
 template <typename TG, int P>
 __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem, TG* dparams, int db, int block) {
     const TileLane t;
@@ -744,15 +745,18 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
     if (n == 0) return;
     const int tiles_v = (n + 255) >> 8, tiles_d = (p.D + 255) >> 8, tiles = tiles_v * tiles_d;
     const int64_t ldz = width;
-    if (block >= tiles) {
-        const int b = block - tiles;
-        if (!db || b >= tiles_v) return;
+    const int pairs = (pl.count + 127) >> 7, per = (pairs + p.dw_splits - 1) / p.dw_splits;
+    const bool whole = p.dw_splits == 1;
+    if (block >= tiles * p.dw_splits) {
+        const int lin = block - tiles * p.dw_splits, split = lin / tiles_v, b = lin - split * tiles_v;
+        if (!db || split >= p.dw_splits) return;
+        const int end = min(pl.count, (split + 1) * per * 128);
         const int c = threadIdx.x & 31, lane_row = threadIdx.x >> 5;
         float s[8] = {};
 #pragma unroll
         for (int part = P - 1; part >= 0; --part) {
             const bf16* src = p.dz + part * p.dz_part + b * 256 + c * 8;
-            for (int r0 = lane_row; r0 < pl.count; r0 += 128) {    // eight rows in flight (up to whole 128 rows, zeros at the end)
+            for (int r0 = split * per * 128 + lane_row; r0 < end; r0 += 128) {    // eight rows in flight (up to whole 128 rows, zeros at the end)
                 u32x4_t v[8];
 #pragma unroll
                 for (int u = 0; u < 8; ++u) v[u] = *reinterpret_cast<const u32x4_t*>(src + (r0 + 16 * u) * ldz);
@@ -773,13 +777,15 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
             float sum = 0.f;
 #pragma unroll
             for (int k = 0; k < 16; ++k) sum += sh[k * 256 + threadIdx.x];
-            dparams[(int64_t)p.V * p.D + v0 + b * 256 + threadIdx.x] = from_f<TG>(sum);
+            const int64_t at = (int64_t)p.V * p.D + v0 + b * 256 + threadIdx.x;
+            if (whole) dparams[at] = from_f<TG>(sum);
+            else p.dw_parts[split * p.dw_stride + at] = sum;
         }
         return;
     }
-    const int tile = xcd_remap(block, tiles);
+    const int lin = xcd_remap(block, tiles * p.dw_splits), split = __builtin_amdgcn_readfirstlane(lin / tiles), tile = lin - split * tiles;
     const int m0 = __builtin_amdgcn_readfirstlane((tile / tiles_d) * 256), n0 = __builtin_amdgcn_readfirstlane((tile % tiles_d) * 256);
-    const int nst = __builtin_amdgcn_readfirstlane(((pl.count + 127) >> 7) * 2);
+    const int first = __builtin_amdgcn_readfirstlane(split * per), nst = __builtin_amdgcn_readfirstlane(min(per, pairs - first)) * 2;
     f32x16_t acc[2][2][2];
     clear(acc);
     if (nst > 0) {
@@ -788,8 +794,8 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
         unsigned vb[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) vb[h] = (unsigned)(t.row_across() * ldb * 2 + min(h * 256 + t.byte_across(), (p.Dp - 8 - n0) * 2));
-        const char* a_base = reinterpret_cast<const char*>(p.dz + m0);
-        const char* b_base = reinterpret_cast<const char*>(p.x + n0);
+        const char* a_base = reinterpret_cast<const char*>(p.dz + first * 128 * ldz + m0);
+        const char* b_base = reinterpret_cast<const char*>(p.x + first * 128 * ldb + n0);
         const Parts<P> parts{nst};
         const int64_t part_a = p.dz_part * 2, part_b = p.Mp * ldb * 2;
         auto issue_a = [&](auto half, int kt, unsigned lds) {
@@ -810,9 +816,10 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         const int v = m0 + j * 128 + t.wn * 32 + t.fr;
-        TG* out = dparams + (int64_t)(v0 + v) * p.D + n0 + t.wm * 64;
-        if constexpr (sizeof(TG) == 4) {
+        const int64_t at = (int64_t)(v0 + v) * p.D + n0 + t.wm * 64;
+        if (sizeof(TG) == 4 || !whole) {
             if (v >= n) continue;
+            float* out = (whole ? reinterpret_cast<float*>(dparams) : p.dw_parts + split * p.dw_stride) + at;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -824,7 +831,8 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
                         if (n0 + t.wm * 64 + d < p.D)
                             *reinterpret_cast<f32x4_t*>(out + d) = f32x4_t{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
                     }
-        } else {
+        } else if constexpr (sizeof(TG) == 2) {
+            TG* out = dparams + at;
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -834,6 +842,24 @@ __device__ __forceinline__ void dw_block(const VocabGemm& p, unsigned char* smem
                 }
         }
     }
+}
+
+// dparams from the sums of the ranges of rows, in their order, four elements per thread.  Bound by reading them.
+template <typename TG>
+__global__ __launch_bounds__(256) void vocab_dw_sum_kernel(const float* __restrict__ parts, int64_t stride, int splits, int64_t n, TG* __restrict__ dparams) {
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at >= n) return;
+    f32x4_t s = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; k += 8) {
+        f32x4_t v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = k + u < splits ? *reinterpret_cast<const f32x4_t*>(parts + (k + u) * stride + at) : f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += v[u];
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (at + e < n) dparams[at + e] = from_f<TG>(s[e]);
 }
 
 // Both, which need dz alone: the first dx_blocks workgroups take dx, whose ranges are the longer ones, and dW's tiles fill the CUs
@@ -886,6 +912,14 @@ int vocab_grads(hipStream_t s, const VocabGemm& p, int64_t dx_blocks, int64_t dw
     if constexpr (sizeof(T) == 2)
         if (grad_bf16) return launch_tiles(vocab_grads_kernel<bf16, 1>, lim[0], dx_blocks + dw_blocks, 512, VG_LDS, s, p, first, (bf16*)dparams, (int)db);
     return launch_tiles(vocab_grads_kernel<float, parts_of<T>>, lim[1], dx_blocks + dw_blocks, 512, VG_LDS, s, p, first, (float*)dparams, (int)db);
+}
+int vocab_dw_sum(hipStream_t s, const VocabGemm& p, void* dparams, bool grad_bf16, int64_t n) {
+    ProfScope ps(K_REDUCE, s, 4.0 * p.dw_splits * n);
+    const dim3 grid((unsigned)((n + 1023) / 1024)), block(256);
+    if (grad_bf16) hipLaunchKernelGGL(vocab_dw_sum_kernel<bf16>, grid, block, 0, s, p.dw_parts, p.dw_stride, p.dw_splits, n, (bf16*)dparams);
+    else hipLaunchKernelGGL(vocab_dw_sum_kernel<float>, grid, block, 0, s, p.dw_parts, p.dw_stride, p.dw_splits, n, (float*)dparams);
+    REV_HIP(hipGetLastError());
+    return REV_OK;
 }
 #define BOTH(T)                                                                                   \
     template int vocab_logits<T>(hipStream_t, const VocabGemm&, bool, bool, bool, int64_t);       \

@@ -17,7 +17,7 @@
 namespace rev {
 
 // What bounds a plan: floats of dz, tiles of 256 columns in dx, places for its ranges (0, 0, 0: there are no tiles); products of
-// parts that make one; whether dW is wanted.
+// parts that make one; ranges of rows of dW, 0 if it is not wanted.
 struct PlanLimits { int64_t dz; int tiles_d, slots, terms, dw; };
 struct RowResults { float* p[4]; };
 
@@ -36,7 +36,8 @@ __device__ __forceinline__ void write_plan(int count, int V, const PlanLimits& l
         if (s <= pairs && tiles * s <= lim.slots) {
             cost = (unsigned)((tiles * s + 255) / 256) * (terms * stages + 10) * 1024 + s;
             if (lim.dw) {
-                const unsigned tile = terms * (p.rows / 64) + 10, all = 4 * tiles * (terms * pairs * 2 + 10 * s) + 3 * (p.width / 256) * lim.tiles_d * tile;
+                const unsigned tile = terms * ((p.rows / 64 + lim.dw - 1) / lim.dw) + 10;
+                const unsigned all = 4 * tiles * (terms * pairs * 2 + 10 * s) + 3 * (p.width / 256) * lim.tiles_d * lim.dw * tile;
                 cost = max(cost, all + 384 * tile);                // half a tile of dW idle at the end
             }
         }
@@ -533,14 +534,18 @@ static int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 // the statistics of a piece in the forward pass, three per 128 entries of a row, or those of 256 entries if that is more
 constexpr int64_t VOCAB_STATS_BYTES = 256 << 20;
+// dW of ranges of rows, all together
+constexpr int64_t VOCAB_DW_BYTES = 256 << 20;
 struct VocabLayout {
-    int64_t plan, flags, place, list, coef, label, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, total;
+    int64_t plan, flags, place, list, coef, label, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, dw_parts, total;
     int64_t Mp, ldz;                 // ldz: of dz in float32
     bool few_f, few_b, few_dz, mid;  // few rows: forward, backward, dz alone; tiles of 128
     int parts;                       // bf16 parts of an operand of the products of tiles
     int Dp, strips, pieces;          // strips of a piece forward; pieces: most that a plan may have backward
     int span;                        // width of a piece forward (tiles of 256)
     int range, ranges, col_groups;   // few_ranges
+    int dw_splits;
+    int64_t dw_stride;
     PlanLimits lim;
 };
 static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
@@ -581,6 +586,11 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
         L.pieces = (int)((V + least - 1) / least);
         L.dz = take(2 * L.parts * L.lim.dz);
         L.acc = take((int64_t)L.lim.slots * 65536 * 4);
+        // dW has as many tiles as the narrowest piece: where these leave CUs without one, ranges of at least 8 stages (6 times 4)
+        L.dw_stride = up(V * D + V, 4);
+        const int64_t tiles_w = std::min(std::max<int64_t>(least, 256), up(V, 256)) / 256 * L.lim.tiles_d;
+        L.dw_splits = (int)std::max<int64_t>(1, std::min({256 / tiles_w, L.Mp / 64 / (L.parts == 1 ? 8 : 4), VOCAB_DW_BYTES / 4 / L.dw_stride}));
+        if (L.dw_splits > 1) L.dw_parts = take(4 * L.dw_splits * L.dw_stride);
     } else {
         L.ldz = up(V, 4);
         few_ranges(c.rows, c.vocab, c.d_model, es, &L.range, &L.ranges, &L.col_groups);
@@ -621,7 +631,7 @@ struct VocabRunner {
     // the rows that count, their logits at named entries, and in the backward pass (cot.lse) what their dense parts are made of
     template <int P> int prepare(const void* X, const RowResults& zero, const Cotangents& cot, bool dw = false) {
         PlanLimits lim = L.lim;
-        lim.dw = dw;
+        lim.dw = dw ? L.dw_splits : 0;
         ProfScope ps(K_CONVERT, s, (double)M * D * 2 * sizeof(T));
         const GatherArgs<T> g = {params, (const T*)X, D, L.Dp, L.Mp, at<void>(L.xc), at<float>(L.zs), cot, cot.lse ? at<float4>(L.coef) : nullptr,
                                  cot.lse && !v.idx ? at<int>(L.label) : nullptr};
@@ -697,6 +707,7 @@ struct VocabRunner {
         RC(gemm_args(&g));
         FewRows<T> f = few_args();
         f.tile_dz = at<bf16>(L.dz);
+        g.dw_parts = at<float>(L.dw_parts); g.dw_stride = L.dw_stride; g.dw_splits = L.dw_splits;
         g.work = 2.0 * M * D * V / L.pieces;                       // (how many of them there are is known to the device)
         f.rows_out = (int)up(M, 128);                              // dW goes over whole 128 rows
         for (int k = 0; k < L.pieces; ++k) {
@@ -706,9 +717,10 @@ struct VocabRunner {
             if (L.few_dz) RC(few_logits<T>(s, f, true, false));
             else RC(vocab_logits<T>(s, g, true, dual(), L.mid, std::min(L.Mp / 256 * tiles_v, std::max(L.lim.dz / 65536, tiles_v))));
             if (v.idx) RC((sparse_dz<bf16, kParts>(k, 0, at<bf16>(L.dz), 0, L.lim.dz)));
-            RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) : 0, dparams,
+            RC(vocab_grads<T>(s, g, dX ? up(L.lim.slots, 8) : 0, dparams ? tiles_v * (L.lim.tiles_d + (c.bias ? 1 : 0)) * L.dw_splits : 0, dparams,
                               c.grad_mode == REV_MODE_BF16, c.bias));
         }
+        if (dparams && L.dw_splits > 1) RC(vocab_dw_sum(s, g, dparams, c.grad_mode == REV_MODE_BF16, (int64_t)V * D + (c.bias ? V : 0)));
         return dX ? vocab_dx_rows<T>(s, g, v.list, v.place, M, dX) : REV_OK;
     }
 

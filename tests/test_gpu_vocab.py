@@ -30,6 +30,14 @@ def test_cross_entropy_in_large_tiles(shape, mode):
     VU.check(VU.make(M, D, V, mode, bias=M % 2 == 1, share=0.8, seed=M), "fp32")
 
 
+@pytest.mark.parametrize("mode,grad", [("bf16", "fp32"), ("bf16", "bf16"), ("fp32", "fp32")])
+@pytest.mark.parametrize("M,D,V,K,share", [(4097, 40, 130, 0, 1.0), (2600, 264, 301, 3, 0.9), (3000, 8, 1, 0, 0.02), (2049, 520, 257, 0, 0.5), (5000, 128, 900, 0, 0.0)])
+def test_many_rows_and_few_weights(M, D, V, K, share, mode, grad):
+    """dW in a few tiles, whose rows are cut into ranges."""
+    print("[case] ranges of rows", M, D, V, K, share, mode, grad, flush=True)
+    VU.check(VU.make(M, D, V, mode, bias=M != 2600, K=K, share=share, seed=M), grad)
+
+
 @pytest.mark.parametrize("mode", ["bf16", "fp32"])
 @pytest.mark.parametrize("K,tau,labels", [(1, 1.0, False), (5, 1.0, True), (33, 2.0, False), (70, 4.0, True)])
 def test_distillation_in_large_tiles(K, tau, labels, mode):
