@@ -252,7 +252,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(
 #pragma unroll
         for (int v = 0; v < 16; ++v) c[v] = 0.f;
     };
-    for (int b = cg * 4 + wave; b < blocks; b += 4 * p.col_groups) {
+    if (const int b = cg * 4 + wave; b < blocks) {
         const int d = b * COLS + CS * fr, dc = min(d, p.D - CS);   // columns beyond D read the last ones again (never stored)
         const T* w = p.w + (int64_t)v0 * p.D;
         // up to 32 rows of x stay in registers
@@ -324,7 +324,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(
                 }
             }
         }
-        if (!want_dx || rows32 == 0) continue;
+        if (!want_dx || rows32 == 0) return;
         constexpr int DB = CS == 2 ? 1 : MB;                       // blocks of 32 rows at a time
         unsigned even[16], odd[16];                                // 32 entries; the next 32, of the range or for the next rows, asked for first
         f32x16_t acc[DB][CS];
@@ -421,14 +421,15 @@ __global__ __launch_bounds__(256) void few_dx_rows_kernel(FewRows<T> p, const in
 // for two workgroups) and, from 5120 entries on, of no fewer than 64, each by as many workgroups as it has groups of four column blocks.  32 rows
 // of 768 to 50265 entries, loss and gradients backward in us by entries per range and groups, bf16 / float32: 224, 2: 126 / 149; 224, 3: 121 / 143; 128,
 // 3: 118 / 157; 64, 3: 129 / 178.  10007 entries in ranges of 32 / 64: 16 bf16 rows of 768 36 / 32, 128 float32 rows of 384 77 / 69.
+// Several groups to a workgroup, 1024 of these / one each: 4 float32 rows of 1544 to 51456 entries 324 / 268, 32 of 728 to 129805 376 / 348, a bf16
+// row of 2048 to 32000 104 / 107.
 void few_ranges(int rows, int V, int D, int es, int* range, int* ranges, int* col_groups) {
     const int blocks32 = (V + 31) / 32, rows32 = (rows + 31) / 32 * 32;
     int per = blocks32 > 160 ? std::max(2, (blocks32 + 319) / 320) : 1;
     while (per > 1 && (per > 8 || rows32 * (per * 32 + 1) * 4 > 72 * 1024)) --per;
     *range = per * 32;
     *ranges = (blocks32 + per - 1) / per;
-    const int groups = ((D * es + 127) / 128 + 3) / 4;             // of four blocks of columns
-    *col_groups = std::max(1, std::min(groups, 1024 / *ranges));
+    *col_groups = ((D * es + 127) / 128 + 3) / 4;                  // of four blocks of columns
 }
 
 template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual) {
