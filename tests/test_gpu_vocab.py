@@ -30,6 +30,16 @@ def test_cross_entropy_in_large_tiles(shape, mode):
     VU.check(VU.make(M, D, V, mode, bias=M % 2 == 1, share=0.8, seed=M), "fp32")
 
 
+# sizes whose logits take tiles of 128 in both passes: more than 800 blocks of 64x64, at most 128 tiles of 256
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("shape,K,tau,labels", [((600, 40, 6001), 0, 1.0, True), ((1100, 72, 3333), 0, 1.0, True), ((520, 64, 7001), 5, 2.0, True),
+                                                ((700, 136, 5121), 3, 0.5, False)])
+def test_in_tiles_of_128(shape, K, tau, labels, mode):
+    M, D, V = shape
+    print("[case] tiles of 128", shape, K, tau, labels, mode, flush=True)
+    VU.check(VU.make(M, D, V, mode, bias=M != 600, K=K, share=0.8, labels=labels, tau=tau, seed=M), "fp32")
+
+
 @pytest.mark.parametrize("mode,grad", [("bf16", "fp32"), ("bf16", "bf16"), ("fp32", "fp32")])
 @pytest.mark.parametrize("M,D,V,K,share", [(4097, 40, 130, 0, 1.0), (2600, 264, 301, 3, 0.9), (3000, 8, 1, 0, 0.02), (2049, 520, 257, 0, 0.5), (5000, 128, 900, 0, 0.0)])
 def test_many_rows_and_few_weights(M, D, V, K, share, mode, grad):
