@@ -399,6 +399,48 @@ def test_captured_and_replayed_with_other_inputs(M, mode):
             assert torch.equal(f[k], eager[k]), (seed, k)
 
 
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("M", [7, 300])
+def test_two_graphs_that_share_a_workspace(M, mode):
+    """Forward and backward captured apart, another problem's call in the same workspace between the replays."""
+    c, d = VU.make(M, 64, 901, mode, K=2, tau=2.0, seed=24), VU.make(M, 64, 901, mode, K=2, tau=2.0, share=0.4, seed=25)
+    cfg, a, b = VU.make_cfg(c), VU.gpu_args(c), VU.gpu_args(d)
+    ws = torch.empty(B.rev_vocab_workspace_bytes(cfg), dtype=torch.uint8, device="cuda")
+    ref = VU.run(c)
+    VU.backward(cfg, c, a, VU.forward(cfg, c, a, workspace=ws)["stats"], workspace=ws)
+    torch.cuda.synchronize()
+    g1, g2 = torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g1):
+        f = VU.forward(cfg, c, a, workspace=ws)
+    with torch.cuda.graph(g2):
+        g = VU.backward(cfg, c, a, f["stats"], workspace=ws)
+    for _ in range(3):
+        g1.replay()
+        VU.backward(cfg, d, b, VU.forward(cfg, d, b, workspace=ws)["stats"], workspace=ws)
+        g2.replay()
+        torch.cuda.synchronize()
+        for k in ref:
+            assert torch.equal(ref[k], (f if k in f else g)[k]), k
+        for t in (*f.values(), *g.values()):
+            t.fill_(3.0)
+
+
+def test_a_stream_given_by_name_and_memory_of_the_call_itself():
+    c = VU.make(300, 128, 1500, "bf16", K=2, seed=26)
+    ref = VU.run(c)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        f = VU.forward(cfg, c, a, stream=side)
+        f.update(VU.backward(cfg, c, a, f["stats"], stream=side))
+        junk = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(4)]      # takes no memory of the calls that run
+        torch.cuda.current_stream().wait_stream(side)
+        for k in ref:
+            assert torch.equal(ref[k], f[k]), k
+        del junk
+
+
 def test_a_row_does_not_depend_on_the_rows_beside_it():
     c = VU.make(400, 128, 2000, "bf16", seed=18)
     one = VU.run(c)
