@@ -215,6 +215,10 @@ __global__ __launch_bounds__(256) void select_gather_kernel(VocabRows v, GatherA
     __shared__ int found[2];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = blockIdx.x;
     const bool first = blockIdx.x == 0;
+    if (i >= v.M) {                                                // a row of zeros in any case
+        gather_row<T, P>(v, g, i, false, 0, 0);
+        return;
+    }
     int f[SELECT_ROWS / 256];
 #pragma unroll
     for (int q = 0; q < SELECT_ROWS / 256; ++q) {
