@@ -397,8 +397,8 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * Workspace.  A copy of the rows that count, and of W in float32 mode or if
  * d_model % 128 != 0 (both go with the number of elements); a piece's dz, at most
  * 512 MB, or 256 entries of all rows if that is more; its statistics, at most
- * 256 MB likewise; fragments of dX in float32.  It does not grow with
- * rows * vocab beyond these.
+ * 256 MB likewise; fragments of dX in float32, and of dW where that is small
+ * (at most 256 MB).  It does not grow with rows * vocab beyond these.
  *
  * Packed parameters: W[vocab, d_model] row-major, then b[vocab] if cfg.bias.
  * dparams: same layout, overwritten.  X, dX: [rows, d_model]; labels, loss,
@@ -407,9 +407,10 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * workspace 256-byte aligned and at least rev_vocab_workspace_bytes() long.
  * Calls enqueue on `stream` and return; nothing is allocated, the workspace may
  * hold anything before a call and is free for others after it, and calls may be
- * captured into a HIP graph.  Sums have a fixed order; a row's loss and dX do not depend on
- * the rows beside it as long as cfg.rows and the number of rows that count stay
- * the same.
+ * captured into a HIP graph.  Sums have a fixed order: a call repeats bit for
+ * bit, and a row's loss and dX do not depend on the rows beside it as long as
+ * cfg.rows and the number of rows that count stay the same.  dX asked for alone
+ * may be summed in another order than beside dparams.
  *
  * Limits (REV_EINVAL otherwise): sizes positive; d_model % 8 == 0 and <= 8192;
  * rows <= 2^20; vocab <= 2^20; 0 <= top_k <= 256; temperature finite and >=
