@@ -44,8 +44,8 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
     const int lane = threadIdx.x & 63, g = lane >> 5, fr = lane & 31;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (!GRAD && (int)blockIdx.x < p.named_blocks) {               // four named entries of a row per wavefront
-        const int per = (p.named.K + 4) >> 2, item = blockIdx.x * 4 + wave, r = item / per;
-        if (r < p.rows) named_logits(p.named, p.x + (int64_t)r * p.ldx, p.w, p.D, r, (item - r * per) * 4, p.zs + (int64_t)r * (p.named.K + 1));
+        const int from = p.named.labels ? 0 : 1, per = (p.named.K + 4 - from) >> 2, item = blockIdx.x * 4 + wave, r = item / per;
+        if (r < p.rows) named_logits(p.named, p.x + (int64_t)r * p.ldx, p.w, p.D, r, from + (item - r * per) * 4, p.zs + (int64_t)r * (p.named.K + 1));
         return;
     }
     const int ahead = GRAD ? 0 : p.named_blocks, tile = xcd_remap(blockIdx.x - ahead, gridDim.x - ahead), nt = tile / p.blocks_m, m0 = (tile - nt * p.blocks_m) * ROWS, n0 = nt * 64;
@@ -438,7 +438,7 @@ template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, boo
     const int tiles = grad && p.tile_dz ? (p.V + 255) / 256 * 4 : (p.V + 63) / 64, covered = grad ? p.rows_out : p.rows;
     const bool one = p.rows <= 32 || (int64_t)((p.rows + 31) / 32) * tiles <= 512;
     p.blocks_m = (covered + (one ? 31 : 63)) / (one ? 32 : 64);
-    p.named_blocks = grad ? 0 : (int)(((int64_t)p.rows * ((p.named.K + 4) >> 2) + 31) / 32 * 8);
+    p.named_blocks = grad ? 0 : (int)(((int64_t)p.rows * ((p.named.K + (p.named.labels ? 4 : 3)) >> 2) + 31) / 32 * 8);
     const dim3 grid((unsigned)(p.named_blocks + p.blocks_m * tiles)), block(256);
 #define FEW1(G, U, MB) do {                                                                                          \
         static LdsLimit lim;                                                                                         \

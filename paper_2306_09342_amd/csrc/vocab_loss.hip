@@ -192,7 +192,7 @@ __device__ __forceinline__ void gather_row(const VocabRows& v, const GatherArgs<
         if (threadIdx.x == 0) g.label[i] = entry_of(v, r, 0);
         return;
     }
-    for (int e0 = (threadIdx.x >> 6) * 4; e0 <= v.K; e0 += 16) named_logits(v, x, g.params, g.D, r, e0, g.zs + (int64_t)i * (v.K + 1));
+    for (int e0 = (threadIdx.x >> 6) * 4 + (v.labels ? 0 : 1); e0 <= v.K; e0 += 16) named_logits(v, x, g.params, g.D, r, e0, g.zs + (int64_t)i * (v.K + 1));
 }
 
 // One workgroup per row of Xc.  Bound by reading the rows of W, scattered over all of it: 64 entries of 8192 rows of 1024, 1.07 GB,
