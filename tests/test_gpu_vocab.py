@@ -32,7 +32,8 @@ def test_cross_entropy_in_large_tiles(shape, mode):
 
 # sizes whose logits take tiles of 128 in both passes: more than 800 blocks of 64x64, at most 128 tiles of 256
 @pytest.mark.parametrize("mode", ["bf16", "fp32"])
-@pytest.mark.parametrize("shape,K,tau,labels", [((600, 40, 6001), 0, 1.0, True), ((1100, 72, 3333), 0, 1.0, True), ((520, 64, 7001), 5, 2.0, True),
+@pytest.mark.parametrize("shape,K,tau,labels", [((600, 40, 6001), 0, 1.0, True), ((1100, 72, 3333), 0, 1.0, True), ((1000, 72, 3333), 4, 2.0, True),
+                                                ((520, 64, 7001), 5, 2.0, True),
                                                 ((700, 136, 5121), 3, 0.5, False)])
 def test_in_tiles_of_128(shape, K, tau, labels, mode):
     M, D, V = shape
