@@ -212,6 +212,19 @@ def _want(t, dtype, shape=None):
         assert tuple(t.shape) == tuple(shape), f"shape {tuple(t.shape)} != {tuple(shape)}"
 
 
+def _new(make, stream, returned=True):
+    """make(): a tensor for a call on `stream`, from that stream's own memory.  A block of the current stream's memory may have been
+    freed while that stream's queued work still uses it, and `stream` does not wait for this.  What is `returned` is kept
+    for the current stream too, where the caller may use it once that stream has waited for the call."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if returned:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def rev_stack_forward(cfg, params, X1, X2, workspace=None, stream=None, Y1=None, Y2=None):
     shape = (cfg.batch, cfg.seq_len, cfg.d_model)
     _want(params, param_dtype(cfg), (rev_stack_param_count(cfg),))
@@ -431,13 +444,11 @@ def rev_vocab_workspace_bytes(cfg: RevVocabCfg) -> int:
     return _check(lib().rev_vocab_workspace_bytes(ctypes.byref(cfg)))
 
 
-def _vocab_new(shape, dtype, X, stream, like=None):
-    """A tensor on the device of X for a call on `stream`: allocated for the current stream, so kept from being used again there before the
-    call's work is done if that is on another one.  `like`: one of the same shape, type and device (the quicker way)."""
-    t = X.new_empty(shape, dtype=dtype) if like is None else torch.empty_like(like)
+def _vocab_new(shape, dtype, X, stream, like=None, returned=True):
+    """A tensor on the device of X for a call on `stream`.  `like`: one of the same shape, type and device (the quicker way)."""
     if stream is not None:
-        t.record_stream(stream)
-    return t
+        return _new(lambda: X.new_empty(shape, dtype=dtype), stream, returned)
+    return X.new_empty(shape, dtype=dtype) if like is None else torch.empty_like(like)
 
 
 def _vocab_want(t, dtype, shape, X):
@@ -457,7 +468,7 @@ def _vocab_common(cfg, params, X, workspace, stream, floats=(), ints=()):
         if t is not None:
             _vocab_want(t, torch.int32, shape, X)
     if workspace is None:
-        return _vocab_new(rev_vocab_workspace_bytes(cfg), torch.uint8, X, stream)
+        return _vocab_new(rev_vocab_workspace_bytes(cfg), torch.uint8, X, stream, returned=False)
     _vocab_want(workspace, torch.uint8, workspace.shape, X)
     return workspace
 
