@@ -230,15 +230,16 @@ def rev_stack_forward(cfg, params, X1, X2, workspace=None, stream=None, Y1=None,
     _want(params, param_dtype(cfg), (rev_stack_param_count(cfg),))
     _want(X1, torch.float32, shape)
     _want(X2, torch.float32, shape)
-    Y1 = torch.empty_like(X1) if Y1 is None else Y1
-    Y2 = torch.empty_like(X2) if Y2 is None else Y2
-    ws = alloc_workspace(cfg, X1.device) if workspace is None else workspace
+    Y1 = _new(lambda: torch.empty_like(X1), stream) if Y1 is None else Y1
+    Y2 = _new(lambda: torch.empty_like(X2), stream) if Y2 is None else Y2
+    ws = _new(lambda: alloc_workspace(cfg, X1.device), stream, returned=False) if workspace is None else workspace
     _check(lib().rev_stack_forward(ctypes.byref(cfg), _ptr(params), _ptr(X1), _ptr(X2), _ptr(Y1), _ptr(Y2),
                                    _ptr(ws), ws.numel(), _stream_handle(stream)))
     return Y1, Y2
 
 
-def _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out):
+def _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream):
+    """stream: that which has all of the call's work behind it once the call returns."""
     shape = (cfg.batch, cfg.seq_len, cfg.d_model)
     _want(params, param_dtype(cfg), (rev_stack_param_count(cfg),))
     for t in (Y1, Y2, dY1, dY2):
@@ -246,18 +247,18 @@ def _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out):
     if out is None:
         out = {}
     dX1 = out.get("dX1", None)
-    dX1 = torch.empty_like(Y1) if dX1 is None else dX1
+    dX1 = _new(lambda: torch.empty_like(Y1), stream) if dX1 is None else dX1
     dX2 = out.get("dX2", None)
-    dX2 = torch.empty_like(Y1) if dX2 is None else dX2
+    dX2 = _new(lambda: torch.empty_like(Y1), stream) if dX2 is None else dX2
     dparams = out.get("dparams", None)
-    dparams = torch.empty(params.numel(), dtype=torch.float32, device=Y1.device) if dparams is None else dparams
+    dparams = _new(lambda: torch.empty(params.numel(), dtype=torch.float32, device=Y1.device), stream) if dparams is None else dparams
     X1o = X2o = None
     if want_inputs:
         X1o = out.get("X1", None)
-        X1o = torch.empty_like(Y1) if X1o is None else X1o
+        X1o = _new(lambda: torch.empty_like(Y1), stream) if X1o is None else X1o
         X2o = out.get("X2", None)
-        X2o = torch.empty_like(Y1) if X2o is None else X2o
-    ws = alloc_workspace(cfg, Y1.device) if workspace is None else workspace
+        X2o = _new(lambda: torch.empty_like(Y1), stream) if X2o is None else X2o
+    ws = _new(lambda: alloc_workspace(cfg, Y1.device), stream, returned=False) if workspace is None else workspace
     res = {"dX1": dX1, "dX2": dX2, "dparams": dparams, "X1": X1o, "X2": X2o}
     args = [ctypes.byref(cfg), _ptr(params), _ptr(Y1), _ptr(Y2), _ptr(dY1), _ptr(dY2), _ptr(dX1), _ptr(dX2),
             _ptr(X1o), _ptr(X2o), _ptr(dparams), _ptr(ws), ws.numel()]
@@ -265,7 +266,7 @@ def _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out):
 
 
 def rev_stack_backward_reprop(cfg, params, Y1, Y2, dY1, dY2, workspace=None, stream=None, want_inputs=False, out=None):
-    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out)
+    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream)
     _check(lib().rev_stack_backward_reprop(*args, _stream_handle(stream)))
     return res
 
@@ -289,7 +290,7 @@ def rev_stack_backward_reprop_static(cfg, params, Y1, Y2, dY1, dY2, out, stream=
 
 def rev_stack_backward_pareprop(cfg, params, Y1, Y2, dY1, dY2, stream_recompute, workspace=None, stream_grad=None,
                                 want_inputs=False, out=None):
-    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out)
+    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream_grad)
     _check(lib().rev_stack_backward_pareprop(*args, _stream_handle(stream_grad), _stream_handle(stream_recompute)))
     return res
 
@@ -305,9 +306,9 @@ def rev_stack_forward_masked(cfg, params, X1, X2, key_len, workspace=None, strea
     _want(X1, torch.float32, shape)
     _want(X2, torch.float32, shape)
     _want_key_len(cfg, key_len)
-    Y1 = torch.empty_like(X1) if Y1 is None else Y1
-    Y2 = torch.empty_like(X2) if Y2 is None else Y2
-    ws = alloc_workspace(cfg, X1.device) if workspace is None else workspace
+    Y1 = _new(lambda: torch.empty_like(X1), stream) if Y1 is None else Y1
+    Y2 = _new(lambda: torch.empty_like(X2), stream) if Y2 is None else Y2
+    ws = _new(lambda: alloc_workspace(cfg, X1.device), stream, returned=False) if workspace is None else workspace
     _check(lib().rev_stack_forward_masked(ctypes.byref(cfg), _ptr(params), _ptr(X1), _ptr(X2), _ptr(key_len), _ptr(Y1),
                                           _ptr(Y2), _ptr(ws), ws.numel(), _stream_handle(stream)))
     return Y1, Y2
@@ -320,7 +321,7 @@ def _masked(args, key_len):
 def rev_stack_backward_reprop_masked(cfg, params, Y1, Y2, key_len, dY1, dY2, workspace=None, stream=None,
                                      want_inputs=False, out=None):
     _want_key_len(cfg, key_len)
-    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out)
+    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream)
     _check(lib().rev_stack_backward_reprop_masked(*_masked(args, key_len), _stream_handle(stream)))
     return res
 
@@ -328,7 +329,7 @@ def rev_stack_backward_reprop_masked(cfg, params, Y1, Y2, key_len, dY1, dY2, wor
 def rev_stack_backward_pareprop_masked(cfg, params, Y1, Y2, key_len, dY1, dY2, stream_recompute, workspace=None,
                                        stream_grad=None, want_inputs=False, out=None):
     _want_key_len(cfg, key_len)
-    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out)
+    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream_grad)
     _check(lib().rev_stack_backward_pareprop_masked(*_masked(args, key_len), _stream_handle(stream_grad),
                                                     _stream_handle(stream_recompute)))
     return res
@@ -336,7 +337,7 @@ def rev_stack_backward_pareprop_masked(cfg, params, Y1, Y2, key_len, dY1, dY2, s
 
 def rev_stack_backward_chain(cfg, params, Y1, Y2, dY1, dY2, chain, workspace=None, stream=None, want_inputs=False,
                              out=None):
-    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out)
+    args, res = _backward_args(cfg, params, Y1, Y2, dY1, dY2, workspace, want_inputs, out, stream)
     _check(lib().rev_stack_backward_chain(*args, _stream_handle(stream), int(chain)))
     return res
 
@@ -390,15 +391,19 @@ def _merge_shapes(cfg):
     return (m_in, cfg.d_in), (m_in // 4, 2 * cfg.d_in)
 
 
+def _merge_workspace(cfg, X1, stream):
+    return _new(lambda: torch.empty(rev_merge_workspace_bytes(cfg), dtype=torch.uint8, device=X1.device), stream, returned=False)
+
+
 def rev_merge_forward(cfg, params, X1, X2, workspace=None, stream=None, out=None):
     """Stage transition: average of the two streams, 2x2 patch merging, LayerNorm, linear map 4C -> 2C."""
     s_in, s_out = _merge_shapes(cfg)
     _want(params, param_dtype(cfg), (rev_merge_param_count(cfg),))
     _want(X1, torch.float32, s_in)
     _want(X2, torch.float32, s_in)
-    out = torch.empty(s_out, dtype=torch.float32, device=X1.device) if out is None else out
+    out = _new(lambda: torch.empty(s_out, dtype=torch.float32, device=X1.device), stream) if out is None else out
     _want(out, torch.float32, s_out)
-    ws = torch.empty(rev_merge_workspace_bytes(cfg), dtype=torch.uint8, device=X1.device) if workspace is None else workspace
+    ws = _merge_workspace(cfg, X1, stream) if workspace is None else workspace
     _check(lib().rev_merge_forward(ctypes.byref(cfg), _ptr(params), _ptr(X1), _ptr(X2), _ptr(out), _ptr(ws), ws.numel(),
                                    _stream_handle(stream)))
     return out
@@ -414,14 +419,14 @@ def rev_merge_backward(cfg, params, X1, X2, dOutA, dOutB, workspace=None, stream
         _want(t, torch.float32, s_out)
     out = {} if out is None else out
     dX1 = out.get("dX1")
-    dX1 = torch.empty_like(X1) if dX1 is None else dX1
+    dX1 = _new(lambda: torch.empty_like(X1), stream) if dX1 is None else dX1
     dX2 = out.get("dX2")
-    dX2 = torch.empty_like(X1) if dX2 is None else dX2
+    dX2 = _new(lambda: torch.empty_like(X1), stream) if dX2 is None else dX2
     dparams = out.get("dparams")
-    dparams = torch.empty(params.numel(), dtype=torch.float32, device=X1.device) if dparams is None else dparams
+    dparams = _new(lambda: torch.empty(params.numel(), dtype=torch.float32, device=X1.device), stream) if dparams is None else dparams
     for t, shp in ((dX1, s_in), (dX2, s_in), (dparams, (params.numel(),))):
         _want(t, torch.float32, shp)
-    ws = torch.empty(rev_merge_workspace_bytes(cfg), dtype=torch.uint8, device=X1.device) if workspace is None else workspace
+    ws = _merge_workspace(cfg, X1, stream) if workspace is None else workspace
     _check(lib().rev_merge_backward(ctypes.byref(cfg), _ptr(params), _ptr(X1), _ptr(X2), _ptr(dOutA), _ptr(dOutB),
                                     _ptr(dX1), _ptr(dX2), _ptr(dparams), _ptr(ws), ws.numel(), _stream_handle(stream)))
     return {"dX1": dX1, "dX2": dX2, "dparams": dparams}

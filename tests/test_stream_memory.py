@@ -31,7 +31,30 @@ def _vocab_call(name, **more):
     return B.rev_distill_backward(VOCAB, i["params"], i["X"], *teacher, i["lse"], i["rows"], labels=i["labels"], dloss_ce=i["rows"], **more)
 
 
+STACK = B.make_cfg(n_blocks=2, d_model=64, n_heads=2, d_mlp=128, seq_len=16, batch=1, mode="bf16")
+MERGE = B.make_merge_cfg(1, 4, 4, 2, 32)
+
+
+def _stack_call(name, stream=None, **more):
+    x, p = torch.zeros(1, 16, 64), torch.zeros(8)
+    key_len = (torch.ones(1).int(),) if name.endswith("_masked") else ()
+    if "forward" in name:
+        return getattr(B, name)(STACK, p, x, x, *key_len, stream=stream, **more)
+    if "pareprop" in name:
+        return getattr(B, name)(STACK, p, x, x, *key_len, x, x, OTHER, stream_grad=stream, want_inputs=True, **more)
+    chain = (1,) if name.endswith("_chain") else ()
+    return getattr(B, name)(STACK, p, x, x, *key_len, x, x, *chain, stream=stream, want_inputs=True, **more)
+
+
+def _merge_call(name, **more):
+    x, y, p = torch.zeros(16, 32), torch.zeros(4, 64), torch.zeros(8)
+    return B.rev_merge_forward(MERGE, p, x, x, **more) if name == "rev_merge_forward" else B.rev_merge_backward(MERGE, p, x, x, y, y, **more)
+
+
 CALLS = {n: _vocab_call for n in ("rev_xent_forward", "rev_xent_backward", "rev_distill_forward", "rev_distill_backward")}
+CALLS.update({"rev_stack_" + n: _stack_call for n in ("forward", "forward_masked", "backward_reprop", "backward_reprop_masked", "backward_pareprop",
+                                                      "backward_pareprop_masked", "backward_chain")})
+CALLS.update({n: _merge_call for n in ("rev_merge_forward", "rev_merge_backward")})
 
 
 @pytest.fixture
