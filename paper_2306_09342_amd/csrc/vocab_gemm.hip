@@ -306,7 +306,7 @@ __device__ __forceinline__ void dz_block(const f32x16_t& z, const float4& c, flo
 }
 __device__ __forceinline__ float4 one_coef(float4 c, int losses) {
     if (losses == LOSS_KD) { c.x = c.z; c.y = c.w; }
-    if (losses == (LOSS_CE | LOSS_KD)) { c.x += c.z; c.y = fminf(c.y, c.w); }    // one of them is 0, or both have one exponential
+    if (losses == (LOSS_CE | LOSS_KD)) { c.x += c.z; c.y = c.y == INFINITY ? c.w : c.y; }    // the one that the row has, NaN too, or both alike
     return c;
 }
 // what replaces the accumulators' start at entry c0 + 8 (v / 4) + v % 4 of a tile that the vocabulary does not fill, or with biased

@@ -499,3 +499,31 @@ def test_a_training_step_through_a_stack_and_the_loss():
     near(b["dX1"], rdx1)
     near(b["dX2"], rdx2)
     near(b["dparams"], O.pack_params(rg))
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("M,V", [(6, 900), (300, 1100), (900, 5001), (900, 17000)])
+def test_an_entry_that_is_not_a_number(M, V, value, tau, mode):
+    """One entry's bias leaves no log-sum-exp: then every dz of a row that counts is no number, whatever of label and teacher the row has."""
+    for have in ("label", "teacher", "both"):
+        c = VU.make(M, 64, V, mode, K=3, tau=tau, seed=30)
+        if have == "label":
+            c["idx"][:] = -1
+        if have == "teacher":
+            c["labels"][:] = -100
+        c["labels"][1] = -100
+        c["idx"][1] = -1                                       # a row that does not count
+        c["params"][V * 64 + V // 2] = value
+        got = VU.run(c)
+        on = (c["labels"] >= 0) | (c["idx"] >= 0).any(1)
+        assert on[2] and not on[1]
+        nan = {k: torch.isnan(v).cpu().numpy() for k, v in got.items()}
+        assert nan["dX"][on].all() and nan["dparams"].all(), have
+        if have != "teacher":
+            assert nan["lse"][on].all() and nan["loss_ce"][on].all(), have
+        if have != "label":
+            assert nan["lse_tau"][on].all() and nan["loss_kd"][on].all(), have
+        for k in ("loss_ce", "loss_kd", "lse", "lse_tau", "dX"):
+            assert not got[k][1].any(), k
