@@ -75,11 +75,12 @@ __device__ __forceinline__ void named_logits(const VocabRows& v, const T* x, con
     }
 }
 
-// The dense part of a row's dz at a logit z: c = {dloss_ce, lse, dloss tau, lse_tau}, {0, infinity} where the row has none.
+// The dense part of a row's dz at a logit z: c = {dloss_ce, lse, dloss tau, lse_tau}, {0, infinity} where the row has none (a cotangent of 0
+// is not that: 0 exp(NaN) stays NaN).
 __device__ __forceinline__ float dense_dz(const float4& c, float z, float inv_tau) {
     float d = 0.f;
-    if (c.x != 0.f) d = c.x * expf(z - c.y);
-    if (c.z != 0.f) d += c.z * expf(z * inv_tau - c.w);
+    if (c.y != INFINITY) d = c.x * expf(z - c.y);
+    if (c.w != INFINITY) d += c.z * expf(z * inv_tau - c.w);
     return d;
 }
 

@@ -527,3 +527,19 @@ def test_an_entry_that_is_not_a_number(M, V, value, tau, mode):
             assert nan["lse_tau"][on].all() and nan["loss_kd"][on].all(), have
         for k in ("loss_ce", "loss_kd", "lse", "lse_tau", "dX"):
             assert not got[k][1].any(), k
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+@pytest.mark.parametrize("M,V", [(6, 900), (300, 1100), (900, 5001), (900, 17000)])
+def test_a_cotangent_of_zero_hides_no_nan(M, V, tau, mode):
+    c = VU.make(M, 64, V, mode, K=3, tau=tau, seed=31)
+    c["labels"][3], c["idx"][4] = -100, -1                     # a teacher alone, a label alone
+    for r in (2, 3, 4):
+        c["X"][r, 7] = np.nan
+        c["dce"][r] = c["dkd"][r] = 0.0
+    c["dce"][5] = c["dkd"][5] = 0.0
+    got = VU.run(c)
+    nan = torch.isnan(got["dX"]).sum(1).cpu().tolist()
+    assert nan[:6] == [0, 0, 64, 64, 64, 0] and not any(nan[6:])
+    assert not got["dX"][5].any() and int(torch.isnan(got["dparams"]).sum()) == V * 65
