@@ -298,7 +298,7 @@ __device__ __forceinline__ void teacher_loss(const VocabRows& v, int r, const fl
     float sum = 0.f;
 #pragma unroll
     for (int q = 0; q < 4; ++q)
-        if (t.p[q] != 0.f) sum += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - top) * v.inv_tau - log_s));
+        if (lane + 64 * q < v.K && t.p[q] != 0.f) sum += t.p[q] * ((t.t[q] - t.log_norm) - ((z[1 + lane + 64 * q] - top) * v.inv_tau - log_s));
     *kd = wave_sum(sum) / (v.inv_tau * v.inv_tau);
     *lse_tau = top * v.inv_tau + log_s;
 }

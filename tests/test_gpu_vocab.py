@@ -543,3 +543,22 @@ def test_a_cotangent_of_zero_hides_no_nan(M, V, tau, mode):
     nan = torch.isnan(got["dX"]).sum(1).cpu().tolist()
     assert nan[:6] == [0, 0, 64, 64, 64, 0] and not any(nan[6:])
     assert not got["dX"][5].any() and int(torch.isnan(got["dparams"]).sum()) == V * 65
+
+
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+@pytest.mark.parametrize("M,V,K", [(6, 900, 3), (7, 900, 70), (300, 1100, 3), (900, 17000, 5)])
+def test_a_teacher_that_is_not_a_number(M, V, K, mode):
+    """NaN or +infinity among a row's teacher logits: no number in that row's divergence, and the last row's too, behind which there are no named logits."""
+    c = VU.make(M, 64, V, mode, K=K, tau=2.0, seed=32)
+    c["idx"][3, 1], c["idx"][M - 1, 0] = 5, 7
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    one = VU.forward(cfg, c, a)
+    one.update(VU.backward(cfg, c, a, one["stats"], want=("dX",)))
+    a["logits"][3, 1], a["logits"][M - 1, 0] = float("nan"), float("inf")
+    two = VU.forward(cfg, c, a)
+    two.update(VU.backward(cfg, c, a, two["stats"], want=("dX",)))
+    for k in ("loss_kd", "dX"):
+        assert torch.isnan(two[k][[3, M - 1]]).all(), k
+        two[k][[3, M - 1]] = one[k][[3, M - 1]]
+    for k in ("loss_ce", "loss_kd", "lse", "lse_tau", "dX"):
+        assert torch.equal(one[k], two[k]), k
