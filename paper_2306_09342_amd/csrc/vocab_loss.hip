@@ -585,7 +585,9 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
         L.lim.dz = L.few_dz ? all : std::min(std::max(VOCAB_DZ_BYTES / 2 / L.parts / 256 * 256, L.Mp * 256), all);
         L.lim.tiles_d = (int)((D + 255) / 256);
         L.lim.terms = L.parts == 1 ? 1 : 6;
-        L.lim.slots = (int)std::max<int64_t>(L.Mp / 256 * L.lim.tiles_d, 512);
+        // places for the ranges of dx: two rounds of tiles, but no more than there can be (write_plan: at most 64, and pairs of stages)
+        const int64_t tiles_x = L.Mp / 256 * L.lim.tiles_d;
+        L.lim.slots = (int)std::max(tiles_x, std::min<int64_t>(512, tiles_x * std::min<int64_t>(64, up(V, 256) / 128)));
         const int64_t least = L.lim.dz / L.Mp / 256 * 256;
         L.pieces = (int)((V + least - 1) / least);
         L.dz = take(2 * L.parts * L.lim.dz);

@@ -102,3 +102,13 @@ def test_the_binding_refuses_other_types_and_shapes():
     with pytest.raises(AssertionError):
         B.rev_xent_forward(c, torch.zeros(B.rev_vocab_param_count(c), dtype=torch.bfloat16), torch.zeros(40, 64, dtype=torch.bfloat16),
                            torch.zeros(40, dtype=torch.int32))            # CPU tensors
+
+
+MB = 1 << 20
+
+
+@pytest.mark.parametrize("mode,rows,d,vocab,most", [("bf16", 129, 64, 200, 2 * MB), ("bf16", 129, 128, 1000, 4 * MB), ("bf16", 300, 64, 17000, 60 * MB),
+                                                    ("fp32", 129, 64, 200, 2 * MB), ("fp32", 900, 64, 5001, 100 * MB)])
+def test_small_problems_have_small_workspaces(mode, rows, d, vocab, most):
+    """No more places for ranges of dX than the ranges that there can be."""
+    assert B.rev_vocab_workspace_bytes(_cfg(rows=rows, d_model=d, vocab=vocab, mode=mode)) <= most
