@@ -143,11 +143,12 @@ template <typename T> struct FewRows {
     const int* label;
     float* dz;                      // [rows_out, ldz], zeros behind the rows that count and the vocabulary
     bf16* tile_dz;                  // the same in bf16, for the products of tiles, in the plan's width; or null
-    float* parts;                   // dx of a range of the vocabulary, [range][rows][D]
+    float* parts;                   // dx of ranges of the vocabulary, [places][rows][D]: the first of `places` ranges, those of the next turn added, ...
     int64_t stat_row, stat_kind, ldz;
     int V, D, ldx, losses, rows_x, rows, rows_out, blocks_m;    // rows: most that count
     int named_blocks;               // workgroups for the named logits, a multiple of 8
     int range, ranges, col_groups;  // entries per range, a multiple of 32
+    int places, first;              // the first range of a turn
     float inv_tau;
 };
 template <typename T> int few_logits(hipStream_t s, FewRows<T> p, bool grad, bool dual);

@@ -190,7 +190,9 @@ __global__ __launch_bounds__(256, 2) void few_logits_kernel(FewRows<T> p) {
 //
 // What bounds it: the float32 matrix cores and the LDS reads of their operands; with one row reading W and writing dW.  768 to 50265
 // entries, float32: one row 67 us (4.6 TB/s of W and dW), 32 rows 87 us.
-template <typename T, typename TG, int MB>
+//
+// ADD: a turn behind the first one, whose dx is added to what is there (a kernel of its own: the loads cost the others registers).
+template <typename T, typename TG, int MB, bool ADD>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(FewRows<T> p, int want_dx, TG* dparams, int db, int apart) {
     constexpr int CS = 4 / sizeof(T), COLS = 32 * CS;              // columns per lane and word; of a block
     extern __shared__ __attribute__((aligned(16))) float dzs[];    // [rows up to whole 32][range + 1], 256 more for db
@@ -204,7 +206,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(
         else { block -= half; dparams = nullptr; }
     }
     const int r = block / p.col_groups, cg = block - r * p.col_groups, P = p.range + 1;
-    const int v0 = r * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
+    const int v0 = (p.first + r) * p.range, nv = min(p.range, p.V - v0), rows32 = (count + 31) & ~31;
     // four entries of a row per thread and load, eight of these in flight (dz has whole quads, zeros behind the vocabulary)
     const int per = p.range >> 2, quads = rows32 * per;
     for (int k0 = threadIdx.x; k0 < quads; k0 += 2048) {
@@ -368,6 +370,10 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(
                         const int i = m0 + m * 32 + 8 * (v >> 2) + 4 * g + (v & 3);
                         if (i >= count) continue;
                         float* out = p.parts + ((int64_t)r * p.rows + i) * p.D + d;
+                        if constexpr (ADD) {
+#pragma unroll
+                            for (int q = 0; q < CS; ++q) acc[m][q][v] += out[q];
+                        }
                         if constexpr (CS == 1) *out = acc[m][0][v];
                         else *reinterpret_cast<float2*>(out) = make_float2(acc[m][0][v], acc[m][1][v]);
                     }
@@ -385,14 +391,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 3) void few_grads_kernel(
     }
 }
 
-// dX[r], 64 columns per workgroup: a sixteenth of the ranges per group of 16 lanes, added in order; zeros for a row that does not count.
+// dX[r], 64 columns per workgroup: a sixteenth of the ranges' places per group of 16 lanes, added in order; zeros for a row that does not count.
 template <typename T>
 __global__ __launch_bounds__(256) void few_dx_rows_kernel(FewRows<T> p, const int* __restrict__ place, T* __restrict__ dX) {
     __shared__ f32x4_t sh[16][16];
     const int r = blockIdx.x, i = place[r], q = threadIdx.x & 15, k = threadIdx.x >> 4, d = blockIdx.y * 64 + q * 4;
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
     if (i >= 0 && d < p.D) {
-        const int per = (p.ranges + 15) >> 4, last = min(p.ranges, (k + 1) * per);
+        const int per = (p.places + 15) >> 4, last = min(p.places, (k + 1) * per);
         const float* at = p.parts + (int64_t)i * p.D + d;
         const int64_t step = (int64_t)p.rows * p.D;
         for (int n = k * per; n < last; n += 8) {
@@ -460,13 +466,21 @@ template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, v
     // Few workgroups wait for memory most of the time: dW and dx in workgroups of their own.  Gradients in us, together / apart: float32, 128 rows,
     // D = 384, V = 1000 (96 workgroups): 34 / 29; 512, 768, 1000 (192): 80 / 71; 333, 200, 5003 (314): 88 / 85; 64, 768, 10007 (939): 80 / 82;
     // bf16, 8, 768, 10007 (939): 35 / 37.
-    const int blocks = p.ranges * p.col_groups, apart = want_dx && dparams && blocks <= 384;
-    const dim3 grid((unsigned)(blocks << apart)), block(256);
-#define GRADS(TG, MB) do {                                                                                             \
+    const int blocks = p.ranges * p.col_groups, apart = want_dx && dparams && blocks <= 384 && p.places == p.ranges;
+    // Turns in float32 only: bf16 calls whose ranges would not all have a place go through tiles (few_backward: at most 21 MB of dx).
+    const int turn = want_dx ? p.places : p.ranges;
+    constexpr bool turns = sizeof(T) == 4;
+#define GRADS1(TG, MB, ADD) do {                                                                                       \
         static LdsLimit lim;                                                                                           \
-        if (int rc = lim.ensure(reinterpret_cast<const void*>(few_grads_kernel<T, TG, MB>), 160 * 1024)) return rc;    \
-        hipLaunchKernelGGL((few_grads_kernel<T, TG, MB>), grid, block, lds, s, p, (int)want_dx, (TG*)dparams, (int)db, apart); \
+        if (int rc = lim.ensure(reinterpret_cast<const void*>(few_grads_kernel<T, TG, MB, ADD>), 160 * 1024)) return rc; \
+        const dim3 grid((unsigned)((std::min(turn, p.ranges - p.first) * p.col_groups) << apart));                     \
+        hipLaunchKernelGGL((few_grads_kernel<T, TG, MB, ADD>), grid, dim3(256), lds, s, p, (int)want_dx, (TG*)dparams, (int)db, apart); \
         REV_HIP(hipGetLastError());                                                                                    \
+    } while (0)
+#define GRADS(TG, MB) do {                                                                                             \
+        p.first = 0;                                                                                                   \
+        GRADS1(TG, MB, false);                                                                                         \
+        for (p.first = turn; turns && p.first < p.ranges; p.first += turn) GRADS1(TG, MB, turns);                      \
         return REV_OK;                                                                                                 \
     } while (0)
     if constexpr (sizeof(T) == 2)
@@ -474,9 +488,10 @@ template <typename T> int few_grads(hipStream_t s, FewRows<T> p, bool want_dx, v
     if (rows32 == 32) GRADS(float, 1);
     GRADS(float, 2);
 #undef GRADS
+#undef GRADS1
 }
 template <typename T> int few_dx_rows(hipStream_t s, const FewRows<T>& p, const int* place, T* dX) {
-    ProfScope ps(K_REDUCE, s, 4.0 * p.ranges * p.rows * p.D);
+    ProfScope ps(K_REDUCE, s, 4.0 * p.places * p.rows * p.D);
     hipLaunchKernelGGL(few_dx_rows_kernel<T>, dim3(p.rows, (p.D + 63) / 64), dim3(256), 0, s, p, place, dX);
     REV_HIP(hipGetLastError());
     return REV_OK;

@@ -540,6 +540,9 @@ constexpr int64_t VOCAB_DZ_BYTES = 512 << 20;
 constexpr int64_t VOCAB_STATS_BYTES = 256 << 20;
 // dW of ranges of rows, all together
 constexpr int64_t VOCAB_DW_BYTES = 256 << 20;
+// dx of few rows' ranges, all together; where there are more, they take turns at these places (a turn is thousands of workgroups then).
+// Backward in ms, a place for each / turns: 64 float32 rows of 4096 to 131072 entries (537 MB) 2.63 / 2.69, 32 of 8192 to 262144 (1.1 GB) 5.99 / 6.04.
+constexpr int64_t VOCAB_FEW_DX_BYTES = 256 << 20;
 struct VocabLayout {
     int64_t plan, flags, place, list, coef, label, zs, stats, carry, xc, w, dz, acc, dzf, parts_dx, dw_parts, total;
     int64_t Mp, ldz;                 // ldz: of dz in float32
@@ -548,6 +551,7 @@ struct VocabLayout {
     int Dp, strips, pieces;          // strips of a piece forward; pieces: most that a plan may have backward
     int span;                        // width of a piece forward (tiles of 256)
     int range, ranges, col_groups;   // few_ranges
+    int places;                      // of ranges of dx
     int dw_splits;
     int64_t dw_stride;
     PlanLimits lim;
@@ -601,7 +605,8 @@ static VocabLayout vocab_layout(const rev_vocab_cfg& c) {
         L.ldz = up(V, 4);
         few_ranges(c.rows, c.vocab, c.d_model, es, &L.range, &L.ranges, &L.col_groups);
         L.dzf = take(4 * M * L.ldz);
-        L.parts_dx = take(4 * (int64_t)L.ranges * M * D);
+        L.places = (int)std::min<int64_t>(L.ranges, VOCAB_FEW_DX_BYTES / 4 / (M * D));
+        L.parts_dx = take(4 * (int64_t)L.places * M * D);
     }
     L.total = at;
     return L;
@@ -675,7 +680,7 @@ struct VocabRunner {
         f.label = v.idx ? nullptr : at<int>(L.label); f.dz = at<float>(L.dzf); f.parts = at<float>(L.parts_dx);
         f.stat_kind = L.strips; f.stat_row = 3 * f.stat_kind; f.ldz = L.ldz;
         f.V = V; f.D = D; f.ldx = L.Dp; f.losses = losses(); f.rows_x = (int)L.Mp; f.rows = f.rows_out = M;
-        f.range = L.range; f.ranges = L.ranges; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
+        f.range = L.range; f.ranges = L.ranges; f.places = L.places; f.col_groups = L.col_groups; f.inv_tau = v.inv_tau;
         return f;
     }
 

@@ -112,3 +112,15 @@ MB = 1 << 20
 def test_small_problems_have_small_workspaces(mode, rows, d, vocab, most):
     """No more places for ranges of dX than the ranges that there can be."""
     assert B.rev_vocab_workspace_bytes(_cfg(rows=rows, d_model=d, vocab=vocab, mode=mode)) <= most
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(64, 8192, 1 << 20), (64, 4096, 131072), (33, 8192, 300000), (1, 8192, 1 << 20), (64, 2048, 32000), (768, 8, 81380),
+                                          (512, 976, 1000)])
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_the_workspace_of_few_rows_is_bounded(rows, d, vocab, mode):
+    """Rows' copy and tables, named logits, dz of the whole vocabulary or of a piece, statistics, fragments of dX and dW, and W where tiles need it laid out."""
+    n = B.rev_vocab_workspace_bytes(_cfg(rows=rows, d_model=d, vocab=vocab, mode=mode))
+    rows_up, d_up = (rows + 255) // 256 * 256, (d + 127) // 128 * 128
+    few = mode == "fp32"                                         # (bf16 of these sizes goes through tiles, and W as it lies)
+    fixed = rows_up * (6 * d_up + 64) + 4 * rows * 5 + 4096
+    assert n <= fixed + (256 * MB if few else 512 * MB) + 32 * MB + 256 * MB + (0 if few else 256 * MB) + (2 * vocab * d_up if d % 128 else 0)
