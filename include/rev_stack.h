@@ -382,7 +382,8 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * A bias of -infinity, or of the type's lowest value, takes an entry out of
  * the vocabulary; one entry has to stay.  Teacher logits may be the lowest
  * value.  An infinity or NaN elsewhere in a row that counts gives NaN where the
- * formulas do, in that row and in dparams.  If no row counts, dparams is 0.
+ * formulas do, in that row and in dparams, whatever its cotangents; a logit of
+ * +infinity leaves its row no log-sum-exp (NaN).  If no row counts, dparams is 0.
  *
  * Types.  REV_MODE_FP32: everything float32.  REV_MODE_BF16: params, X and dX
  * bfloat16; dparams float32 or bfloat16 (cfg.grad_mode).  Logits, softmax
@@ -394,11 +395,13 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * entry's logits where float32 would have an infinity.  loss, lse, dloss and
  * teacher_logits are float32, labels and teacher_idx int32.
  *
- * Workspace.  A copy of the rows that count, and of W in float32 mode or if
- * d_model % 128 != 0 (both go with the number of elements); a piece's dz, at most
- * 512 MB, or 256 entries of all rows if that is more; its statistics, at most
- * 256 MB likewise; fragments of dX in float32, and of dW where that is small
- * (at most 256 MB).  It does not grow with rows * vocab beyond these.
+ * Workspace.  What goes with the number of elements: a copy of the rows (2 bytes
+ * an element in bf16 mode, 6 in float32); one of W alike, in float32 mode or if
+ * d_model % 128 != 0, unless rows are few; a dX in float32; and rows * (top_k + 1)
+ * logits of labels and teacher entries.  Besides these, at most 512 MB for dz of a
+ * piece of the vocabulary, or 256 entries of all rows if that is more (few rows: of
+ * the whole vocabulary, 256 MB); 256 MB for a piece's statistics, likewise; and 256 MB
+ * each for fragments of dX and of dW, whose sums are the results.
  *
  * Packed parameters: W[vocab, d_model] row-major, then b[vocab] if cfg.bias.
  * dparams: same layout, overwritten.  X, dX: [rows, d_model]; labels, loss,

@@ -124,3 +124,20 @@ def test_the_workspace_of_few_rows_is_bounded(rows, d, vocab, mode):
     few = mode == "fp32"                                         # (bf16 of these sizes goes through tiles, and W as it lies)
     fixed = rows_up * (6 * d_up + 64) + 4 * rows * 5 + 4096
     assert n <= fixed + (256 * MB if few else 512 * MB) + 32 * MB + 256 * MB + (0 if few else 256 * MB) + (2 * vocab * d_up if d % 128 else 0)
+
+
+@pytest.mark.parametrize("rows,d,vocab", [(8192, 1024, 131072), (65536, 1024, 131072), (4096, 64, 1 << 20), (1 << 20, 8, 50265), (1 << 20, 8192, 1 << 20), (16384, 768, 50265),
+                                          (2500, 200, 1 << 20), (769, 128, 900000), (1000, 8192, 300), (129, 64, 50265)])
+@pytest.mark.parametrize("top_k", [0, 256])
+@pytest.mark.parametrize("mode", ["bf16", "fp32"])
+def test_the_workspace_is_what_the_header_says(rows, d, vocab, top_k, mode):
+    """Its parts one by one, each at its bound; where the logits of all rows would be larger than that, they are not in it."""
+    n = B.rev_vocab_workspace_bytes(_cfg(rows=rows, d_model=d, vocab=vocab, mode=mode, top_k=top_k))
+    rows_up, d_up, e = (rows + 255) // 256 * 256, (d + 127) // 128 * 128, 2 if mode == "bf16" else 6
+    copies = rows_up * e * d_up + (e * vocab * d_up if mode == "fp32" or d % 128 else 0) + 4 * rows_up * ((d + 255) // 256 * 256)
+    tables = 64 * rows_up + 4 * rows * (top_k + 1) + 4096
+    pieces = max(512 * MB, 256 * e * rows_up) + max(256 * MB, 24 * rows_up)
+    assert n <= copies + tables + pieces + 2 * 256 * MB
+    # the logits at two bytes each would not fit beside what goes with the elements
+    if 2 * rows * vocab > pieces + 2 * 256 * MB:
+        assert n < copies + tables + 2 * rows * vocab
