@@ -41,9 +41,10 @@ def reference(c, a, grad_mode):
     top = z.abs().amax(1)
     dz, Edz, out = torch.zeros_like(z), torch.zeros_like(z), {}
     for name, lname, active, t in (("loss_ce", "lse", has, 1.0), ("loss_kd", "lse_tau", taught, tau)):
-        if (a["labels"] if name == "loss_ce" else a["idx"]) is None:
-            continue
         zero = torch.zeros(M, dtype=torch.float64, device="cuda")
+        if (a["labels"] if name == "loss_ce" else a["idx"]) is None:
+            out[lname] = zero, zero
+            continue
         lse = torch.logsumexp(z / t, 1)
         El = Ez.amax(1) / t + (V / 8 + 64 + 4 * np.log(V) + 8 * top / t + 4 * lse.abs()) * U
         out[lname] = torch.where(active, lse, zero), torch.where(active, El, zero)
