@@ -388,8 +388,8 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * Types.  REV_MODE_FP32: everything float32.  REV_MODE_BF16: params, X and dX
  * bfloat16; dparams float32 or bfloat16 (cfg.grad_mode).  Logits, softmax
  * statistics and all sums are float32 in both modes; in bf16 mode dz is rounded
- * to bfloat16 once, as an operand of the two products (for few rows not at
- * all).  In float32 mode the products of more than a few rows take every operand
+ * to bfloat16 once, as an operand of the two products, for float32 dparams too
+ * (for few rows not at all).  In float32 mode the products of more than a few rows take every operand
  * as a sum of three bfloat16 values, which leaves out 2^-23 of |x||w| of a
  * product; there, an infinite weight, or one beyond 3.39e38, gives NaN in its
  * entry's logits where float32 would have an infinity.  loss, lse, dloss and
