@@ -389,11 +389,11 @@ int rev_merge_backward(const rev_merge_cfg* cfg, const void* params,
  * bfloat16; dparams float32 or bfloat16 (cfg.grad_mode).  Logits, softmax
  * statistics and all sums are float32 in both modes; in bf16 mode dz is rounded
  * to bfloat16 once, as an operand of the two products, for float32 dparams too
- * (for few rows not at all).  In float32 mode the products of more than a few rows take every operand
- * as a sum of three bfloat16 values, which leaves out 2^-23 of |x||w| of a
- * product; there, an infinite weight, or one beyond 3.39e38, gives NaN in its
- * entry's logits where float32 would have an infinity.  loss, lse, dloss and
- * teacher_logits are float32, labels and teacher_idx int32.
+ * (for few rows not at all).  In float32 mode the products of more than a few
+ * rows take every operand as a sum of three bfloat16 values, which leaves out
+ * 2^-23 of |x||w| of a product; there, an infinite weight, or one beyond 3.39e38,
+ * gives NaN in its entry's logits where float32 would have an infinity.  loss,
+ * lse, dloss and teacher_logits are float32, labels and teacher_idx int32.
  *
  * Workspace.  What goes with the number of elements: a copy of the rows (2 bytes
  * an element in bf16 mode, 6 in float32); one of W alike, in float32 mode or if

@@ -82,3 +82,26 @@ def test_stage_transition(mode):
         _queue_work_on_freed_memory()
         for a, b in zip(ref, run(side)):
             assert torch.equal(a, b)
+
+
+def test_a_stream_that_joins_a_capture():
+    """Calls on a stream forked from the captured one, in memory of their own: replays repeat the eager results."""
+    c = VU.make(300, 128, 1500, "bf16", K=2, tau=2.0, seed=27)
+    ref = VU.run(c)
+    cfg, a = VU.make_cfg(c), VU.gpu_args(c)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        f = VU.forward(cfg, c, a, stream=side)
+        f.update(VU.backward(cfg, c, a, f["stats"], stream=side))
+        torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        graph.replay()
+        VU.run(c)
+        torch.cuda.synchronize()
+        for k in ref:
+            assert torch.equal(ref[k], f[k]), k
+        for t in f.values():
+            t.fill_(3.0)

@@ -110,4 +110,4 @@ def check(c, a, got, ref, grad_mode="fp32"):
         assert bool(((e <= lim) | (e < 1e-35)).all()), f"{k}: {float((e / lim.clamp(min=1e-300)).max()):.3g} times what rounding allows"
         norm = float(torch.linalg.norm(terms if k == "loss_kd" else want))
         tol = 4 * VU.HALF["bf16"] if "bf16" in (c["mode"], grad_mode) and k in ("dX", "dparams") else 2e-5
-        assert float(torch.linalg.norm(e)) <= tol * norm, f"{k}: relative error {float(torch.linalg.norm(e)) / norm:.3g}"
+        assert norm == 0 or float(torch.linalg.norm(e)) <= tol * norm, f"{k}: relative error {float(torch.linalg.norm(e)) / norm:.3g}"
